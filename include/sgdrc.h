@@ -44,6 +44,11 @@
  *  - A context serves one device.  It may be used from several host
  *    threads; operations on one stream are ordered, operations on different
  *    streams may run concurrently (each stream gets its own work queue).
+ *  - The cache calls (colored_kv_map, colored_kv_append, colored_kv_commit,
+ *    colored_tree_attention) enqueue kernels only and may be captured too.
+ *    What the host cannot know -- lengths, slots, block tables -- they read
+ *    on the device and check there: what is out of range is skipped and
+ *    raises SGDRC_DEVERR_SEQ (pages: SGDRC_DEVERR_PT_RANGE).
  *  - CU masks (set_cu_mask) confine every tile of work to the allowed CUs.
  *    A launch's remainder below the 16-byte access granularity (the last
  *    n mod 16 bytes of a relayout or triad, the last n mod 16 addresses of
@@ -80,6 +85,8 @@ extern "C" {
 #define SGDRC_DEVERR_SUSPENDED_DROPPED 4u  /* a suspended launch was discarded unresumed */
 #define SGDRC_DEVERR_HANDBACK 8u           /* a handed-back tile index out of range (skipped;
                                             * a library fault, never expected) */
+#define SGDRC_DEVERR_SEQ 16u               /* a length, row start, slot or path of a cache call out of
+                                            * range (skipped) */
 
 /* element encodings */
 enum { SGDRC_F32 = 0, SGDRC_BF16 = 1, SGDRC_F16 = 2 };
@@ -476,6 +483,168 @@ enum { SGDRC_GEMV_BY_TILES = 0, SGDRC_GEMV_RING = 1, SGDRC_GEMV_STREAM = 2 };
 int colored_gemv_form(uint32_t allowed_cus, uint32_t schedule, int w_dtype, uint32_t M, uint32_t K,
                       int x_dtype, uint32_t batch, uint32_t page_shift, uint32_t *form,
                       uint32_t *loads);
+
+/* ---------------------------------------------------- key/value cache
+ *
+ * The state of decoding on coloured pages.  A cache is a pool whose pages
+ * each hold one block of block_tokens tokens; the pages of a request are
+ * listed in its row of a block table (entry b: the pool page of tokens
+ * b * block_tokens ...), and slot = page * block_tokens + offset names a
+ * token's place.  The pages come from a ring of free pages, which a page
+ * table of chosen colours fills (colour_alloc_pagetable).
+ *
+ * Inside a page, layer l's block begins at l * layer_stride bytes; there,
+ * key/value head h has 2 * block_tokens * head_dim elements at h times that
+ * many: K as [head_dim / 8][block_tokens][8 dims], then V as
+ * [block_tokens / 8][head_dim][8 tokens].  (16 bytes are what one lane of a
+ * matrix instruction takes of K, along the head, and of V, along the tokens;
+ * so both go from memory to the instruction's registers unchanged.)
+ *
+ * A step of decoding with drafts: colored_kv_map gives every request the
+ * pages for its new tokens and every token its slot; for each layer,
+ * colored_kv_append writes K and V and colored_tree_attention reads them;
+ * once the accepted path of each draft is known, colored_kv_commit closes it
+ * up in all layers.  Lengths and states are double-buffered: each call reads
+ * one set and writes another. */
+#define SGDRC_MAX_REQUESTS 4096
+#define SGDRC_MAX_NODES 256
+#define SGDRC_MAX_KV_HEADS 256
+#define SGDRC_MAX_HEADS 1024
+
+/* A cache.  layer_stride: either the layers' blocks lie in each page one
+ * after another (n_layers * layer_stride <= 2^page_shift), or every layer has
+ * a pool of its own (layer_stride >= pool_pages * 2^page_shift).  A multiple
+ * of 256.  dtype: SGDRC_BF16 or SGDRC_F16.  head_dim: 64, 96, 128 or 256.
+ * block_tokens: a power of two, 16..1024.  A block of one layer,
+ * 4 * kv_heads * block_tokens * head_dim bytes, must fit its layer_stride
+ * (with one layer: its page). */
+typedef struct {
+    void *pool;            /* 256-byte aligned */
+    uint64_t pool_pages;
+    uint64_t layer_stride; /* bytes */
+    uint32_t n_layers;
+    uint32_t page_shift;
+    uint32_t block_tokens;
+    uint32_t kv_heads;
+    uint32_t head_dim;
+    uint32_t dtype;
+} sgdrc_kv_cache;
+
+/* Block tables: row r of ``stride`` entries is request r's (device). */
+typedef struct {
+    uint32_t *table;
+    uint32_t stride;
+    uint32_t n_requests;   /* 1..4096 */
+} sgdrc_kv_blocks;
+
+/* Rows of heads: element d of head h of token t is at
+ * ptr[t * token_stride + h * head_stride + d] (strides in elements, multiples
+ * of 8; ptr 16-byte aligned), so that a slice of a wider projection can be
+ * passed as it is. */
+typedef struct {
+    void *ptr;
+    uint64_t token_stride;
+    uint64_t head_stride;
+} sgdrc_rows;
+
+/* What is kept for the requests between steps (device): how many pages were
+ * taken from the ring and put there since it was made (ring[i mod size] for
+ * taken <= i < put are the free ones), the blocks in each request's row of
+ * the table, and the tokens in its cache. */
+typedef struct {
+    uint64_t *ring_pos;  /* {taken, put} */
+    int32_t *held;
+    int32_t *lens;
+} sgdrc_kv_state;
+
+/* Block tables and slot maps of a step, from the requests' lengths.  Request
+ * r gets d_new[r] >= 0 new tokens: the blocks that they need beyond held[r]
+ * are taken from d_ring in request order and entered in its row, its tokens'
+ * slots go to d_slots in request order, and d_q_start[r] (n_requests + 1
+ * entries) is the first of them; d_request and d_position receive each
+ * token's request and its place in the sequence.  Entries of these three at
+ * and beyond d_q_start[n_requests] are set to -1.  A request that
+ * needs pages is served if the ring holds those of all requests up to it;
+ * otherwise its length and blocks stay and its tokens' slots are -1.
+ * d_new[r] < 0 ends request r: its pages go back to the ring (to be taken
+ * from the next call on), its length and blocks become 0; where the ring, as
+ * it was before the call, has no room for the pages of all ended requests up
+ * to it, the request keeps its state and raises SGDRC_DEVERR_SEQ.  Reads ``in``,
+ * writes ``out``; the two must not share memory.  A request whose state is out
+ * of range, whose tokens pass its table row or n_tokens, keeps its state, gets
+ * slots -1 and raises SGDRC_DEVERR_SEQ; d_q_start is capped at n_tokens.
+ * ring_size: at least the pages in circulation.  n_tokens: entries of
+ * d_slots, d_request and d_position (0 is valid, with those NULL).  EINVAL: NULL or misaligned
+ * pointers, in and out sharing a pointer, block_tokens not a power of two in
+ * 16..1024, n_requests outside 1..4096, stride * block_tokens above 2^31 - 1,
+ * ring_size 0, n_tokens above 2^31 - 1. */
+int colored_kv_map(sgdrc_ctx *ctx, uint32_t block_tokens, const sgdrc_kv_state *in,
+                   const sgdrc_kv_state *out, uint32_t *d_ring, uint32_t ring_size,
+                   const sgdrc_kv_blocks *blocks, const int32_t *d_new, uint32_t *d_q_start,
+                   int64_t *d_slots, int32_t *d_request, int32_t *d_position, uint32_t n_tokens,
+                   void *stream);
+
+/* Writes the K and V rows of n_tokens tokens (kv_heads heads each, of the
+ * cache's dtype) to their slots in layer ``layer``; slot -1: nowhere.  No two
+ * tokens may have the same slot.  n_tokens == 0 launches nothing.  EINVAL: a
+ * bad cache, layer, NULL or misaligned pointers or strides, too many tokens
+ * (n_tokens * kv_heads / 16 above 2^31). */
+int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer,
+                      const sgdrc_rows *k, const sgdrc_rows *v, const int64_t *d_slots,
+                      uint32_t n_tokens, void *stream);
+
+/* Closes up the accepted path of each request's draft, in every layer: the
+ * token at d_lens[r] + path[i] moves to d_lens[r] + i for i < d_accepted[r],
+ * path = d_path + r * path_stride strictly ascending, from 0 on.  Then
+ * d_lens_out[r] = d_lens[r] + d_accepted[r] (d_lens_out must not be d_lens).
+ * Tokens past the path keep what they hold.  A path that does not ascend, is
+ * longer than path_stride or leaves the table's row is cut there, and raises
+ * SGDRC_DEVERR_SEQ.  EINVAL: a bad cache, NULL or misaligned pointers,
+ * path_stride outside 1..256, as colored_kv_map for the blocks. */
+int colored_kv_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks,
+                      const int32_t *d_lens, const int32_t *d_path, uint32_t path_stride,
+                      const int32_t *d_accepted, int32_t *d_lens_out, void *stream);
+
+/* Attention of each request's new tokens, the nodes of a tree of drafted
+ * tokens, over its cache.  Request r's nodes are the tokens
+ * d_q_start[r] .. d_q_start[r + 1] - 1 of q; its cache holds d_totals[r] tokens,
+ * of which the first d_lens[r] are seen by all nodes, and token
+ * d_lens[r] + j by node i if bit j of node i's mask is set (d_mask: mask_words
+ * 64-bit words for each token of q, bit j of a row in word j / 64) or, with
+ * d_mask NULL, if j <= i: a chain, of which a single token is the shortest.
+ * Query head h reads key/value head h / (n_heads / kv_heads).  With
+ *   s_ij = scale q_i . k_j, capped to softcap tanh(s_ij / softcap) if
+ *   softcap > 0,
+ * o_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij) over the tokens j that node i
+ * sees, rounded to the cache's dtype, and d_lse (nullable; [n_tokens][n_heads]
+ * fp32) receives log sum_j exp(s_ij).  A node that sees nothing gets zeros and
+ * -infinity.  What a token that a node does not see holds, NaN and infinity
+ * too, does not reach that node.  Scores, maxima and sums are fp32; exp(s)
+ * is rounded to the cache's dtype where it is multiplied by V.  The order of
+ * all sums depends on the lengths and shapes only, never on the CU mask:
+ * results are bitwise reproducible.  Rows of tokens outside every request
+ * are not written.
+ * d_work: work_bytes of device memory, 256-byte aligned, at least
+ * sgdrc_tree_attention_workspace's; used by the call until it is done, holds
+ * nothing between calls.  max_nodes: no request has more nodes (those beyond
+ * are not computed and raise SGDRC_DEVERR_SEQ).  EINVAL: a bad cache or layer,
+ * n_heads not a multiple of kv_heads or above 1024, max_nodes outside 1..256, mask_words 0
+ * or above 4 with a mask, scale not positive and finite, softcap negative or
+ * not finite, NULL or misaligned pointers or strides, a workspace too small,
+ * as colored_kv_map for the blocks; more than 2^31 steps of 32 tokens over
+ * all requests at full tables.  n_tokens == 0 launches nothing. */
+int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer,
+                           const sgdrc_rows *q, uint32_t n_heads, const uint32_t *d_q_start,
+                           uint32_t n_tokens, uint32_t max_nodes, const sgdrc_kv_blocks *blocks,
+                           const int32_t *d_lens, const int32_t *d_totals, const uint64_t *d_mask,
+                           uint32_t mask_words, float scale, float softcap, const sgdrc_rows *o,
+                           float *d_lse, void *d_work, uint64_t work_bytes, void *stream);
+
+/* Bytes of workspace that colored_tree_attention needs for up to max_nodes
+ * nodes a request and n_heads heads on this cache, whatever the lengths and
+ * the number of requests (host-only, no context).  EINVAL: as there, NULL bytes. */
+int sgdrc_tree_attention_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads,
+                                   uint32_t max_nodes, uint64_t *bytes);
 
 /* ---------------------------------------------------- bimodal tensors
  *

@@ -23,6 +23,7 @@ DEVERR_PT_RANGE = 1
 DEVFLAG_GATE_FALLBACK = 2
 DEVERR_SUSPENDED_DROPPED = 4
 DEVERR_HANDBACK = 8
+DEVERR_SEQ = 16
 MAX_MASKS = 8
 BM_BE_WEIGHT, BM_LS_TENSOR, BM_ACTIVATION = 0, 1, 2
 BM_MONOPOLY, BM_COLOCATED = 0, 1
@@ -71,6 +72,24 @@ GEMV_VALU, GEMV_MFMA = 0, 1
 class RelayoutItem(ctypes.Structure):
     _fields_ = [("dst", Paged), ("src", Paged), ("n_bytes", ctypes.c_uint64),
                 ("page_shift", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("pool_pages", ctypes.c_uint64), ("layer_stride", ctypes.c_uint64),
+                ("n_layers", ctypes.c_uint32), ("page_shift", ctypes.c_uint32), ("block_tokens", ctypes.c_uint32),
+                ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("dtype", ctypes.c_uint32)]
+
+
+class KvBlocks(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("stride", ctypes.c_uint32), ("n_requests", ctypes.c_uint32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class KvState(ctypes.Structure):
+    _fields_ = [("ring_pos", ctypes.c_void_p), ("held", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
 
 
 _lib = None
@@ -128,6 +147,13 @@ def lib() -> ctypes.CDLL:
             "colored_gemv": ([vp, P(Paged), i32, u32, u32, vp, i32, u32, vp, u32, vp], i32),
             "colored_gemv_plan": ([u32, i32, u32, u32, i32, u32, P(GemvPlan)], i32),
             "colored_gemv_form": ([u32, u32, i32, u32, u32, i32, u32, u32, P(u32), P(u32)], i32),
+            "colored_kv_map": ([vp, u32, P(KvState), P(KvState), vp, u32, P(KvBlocks), vp, vp, vp, vp, vp, u32, vp],
+                               i32),
+            "colored_kv_append": ([vp, P(KvCache), u32, P(Rows), P(Rows), vp, u32, vp], i32),
+            "colored_kv_commit": ([vp, P(KvCache), P(KvBlocks), vp, vp, u32, vp, vp, vp], i32),
+            "colored_tree_attention": ([vp, P(KvCache), u32, P(Rows), u32, vp, u32, u32, P(KvBlocks), vp, vp, vp, u32,
+                                        ctypes.c_float, ctypes.c_float, P(Rows), vp, vp, u64, vp], i32),
+            "sgdrc_tree_attention_workspace": ([P(KvCache), u32, u32, P(u64)], i32),
             "colour_classify_table": ([vp, P(ColourTable), vp, u64, vp, vp, vp], i32),
             "colour_alloc_pagetable_table": ([vp, P(ColourTable), u64, u32, u64, P(ColourSet), u64,
                                               vp, P(u64), vp], i32),
@@ -455,6 +481,126 @@ def gemv_form(allowed_cus: int, schedule: str, w_dtype: int, M: int, K: int, x_d
                                    int(K), int(x_dtype), int(batch), int(page_shift), ctypes.byref(form),
                                    ctypes.byref(loads)))
     return ("tiles", "ring", "stream")[form.value], loads.value
+
+
+def kv_cache(pool, pool_pages: int, page_shift: int, block_tokens: int, kv_heads: int, head_dim: int, dtype: int,
+             n_layers: int = 1, layer_stride: int = 0) -> KvCache:
+    """Descriptor of a paged key/value cache (sgdrc_kv_cache); it keeps a
+    reference to ``pool``."""
+    c = KvCache(_addr(pool), int(pool_pages), int(layer_stride), int(n_layers), int(page_shift), int(block_tokens),
+                int(kv_heads), int(head_dim), int(dtype))
+    c._keep = pool
+    return c
+
+
+def _ints_of(t, name: str, size: int = 4):
+    """Device address of a contiguous tensor of ``size``-byte whole numbers."""
+    if t is None or not hasattr(t, "data_ptr"):
+        return _addr(t)
+    if t.element_size() != size or t.is_floating_point() or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {8 * size}-bit whole numbers")
+    return t.data_ptr()
+
+
+def _blocks(table) -> KvBlocks:
+    if table.dim() != 2 or table.element_size() != 4 or table.is_floating_point() or table.stride(1) != 1:
+        raise ValueError("table must be [requests, blocks] of 32-bit whole numbers, rows without gaps inside")
+    n = table.shape[0]
+    return KvBlocks(table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], n)
+
+
+def _rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
+    """Rows of heads of a [tokens, heads, dim] tensor, the last dimension without gaps."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or (t.stride(2) != 1 and t.numel()):
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], the last dimension contiguous")
+    if (F32, BF16, F16)[dtype] != _dtype_of(t):
+        raise ValueError(f"{name} is not of the cache's dtype")
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _dtype_of(t) -> int:
+    return {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}.get(str(t.dtype), -1)
+
+
+def colored_kv_map(ctx, block_tokens: int, ring, ring_pos, held, lens, new, table, ring_pos_out, held_out, lens_out,
+                   q_start, slots, request, position, stream=None) -> None:
+    """Block tables and slot maps of a step from the requests' lengths: the
+    state (ring_pos, held, lens) is read and the next one written to
+    (ring_pos_out, held_out, lens_out); ``new`` holds each request's new tokens
+    (-1: the request ends), ``table`` [requests, blocks] is updated, and
+    ``slots`` (int64), ``request`` and ``position`` (int32) receive an entry a
+    token, -1 past the last."""
+    blocks = _blocks(table)
+    n, tokens = blocks.n_requests, slots.numel()
+    if not (held.numel() == lens.numel() == new.numel() == held_out.numel() == lens_out.numel() == n
+            and q_start.numel() == n + 1 and request.numel() == position.numel() == tokens
+            and ring_pos.numel() == ring_pos_out.numel() == 2):
+        raise ValueError("the arrays' lengths do not fit the table's requests and each other")
+    before = KvState(_ints_of(ring_pos, "ring_pos", 8), _ints_of(held, "held"), _ints_of(lens, "lens"))
+    after = KvState(_ints_of(ring_pos_out, "ring_pos_out", 8), _ints_of(held_out, "held_out"),
+                    _ints_of(lens_out, "lens_out"))
+    _check(lib().colored_kv_map(_h(ctx), int(block_tokens), before, after, _ints_of(ring, "ring"), ring.numel(),
+                                blocks, _ints_of(new, "new"), _ints_of(q_start, "q_start"),
+                                _ints_of(slots, "slots", 8), _ints_of(request, "request"),
+                                _ints_of(position, "position"), tokens, _stream(stream)))
+
+
+def colored_kv_append(ctx, cache: KvCache, layer: int, k, v, slots, stream=None) -> None:
+    """Writes k and v ([tokens, kv_heads, head_dim]) to the cache's ``slots`` (int64, -1: nowhere)."""
+    n = slots.numel()
+    if k.shape[0] != n or v.shape[0] != n:
+        raise ValueError("k, v and slots must have as many tokens")
+    _check(lib().colored_kv_append(_h(ctx), cache, int(layer),
+                                   _rows(k, "k", cache.kv_heads, cache.head_dim, cache.dtype),
+                                   _rows(v, "v", cache.kv_heads, cache.head_dim, cache.dtype),
+                                   _ints_of(slots, "slots", 8), n, _stream(stream)))
+
+
+def colored_kv_commit(ctx, cache: KvCache, table, lens, path, accepted, lens_out, stream=None) -> None:
+    """Closes up each request's accepted path (``path`` [requests, most], the
+    first ``accepted`` entries of a row) in all layers; lens_out = lens + accepted."""
+    blocks = _blocks(table)
+    n = blocks.n_requests
+    if not (lens.numel() == accepted.numel() == lens_out.numel() == n and path.dim() == 2 and path.shape[0] == n):
+        raise ValueError("the arrays' lengths do not fit the table's requests")
+    _check(lib().colored_kv_commit(_h(ctx), cache, blocks, _ints_of(lens, "lens"), _ints_of(path, "path"),
+                                   path.shape[1], _ints_of(accepted, "accepted"), _ints_of(lens_out, "lens_out"),
+                                   _stream(stream)))
+
+
+def tree_attention_workspace(cache: KvCache, n_heads: int, max_nodes: int) -> int:
+    """Bytes of workspace that colored_tree_attention needs (host-only; no device needed)."""
+    n = ctypes.c_uint64()
+    _check(lib().sgdrc_tree_attention_workspace(cache, int(n_heads), int(max_nodes), n))
+    return n.value
+
+
+def colored_tree_attention(ctx, cache: KvCache, layer: int, q, q_start, table, lens, totals, out, work, lse=None,
+                           mask=None, max_nodes: int = 1, scale: float = 1.0, softcap: float = 0.0,
+                           stream=None) -> None:
+    """Attention of each request's nodes (tokens q_start[r] .. q_start[r + 1] of
+    ``q`` [tokens, heads, head_dim]) over its cache: ``lens`` tokens seen by all,
+    and of the drafted ones up to ``totals`` those whose bit is set in the
+    node's row of ``mask`` ([tokens, words] int64; None: a chain).  Writes
+    ``out`` (as q) and, if given, ``lse`` ([tokens, heads] fp32)."""
+    blocks = _blocks(table)
+    n, (tokens, heads) = blocks.n_requests, q.shape[:2]
+    if not (lens.numel() == totals.numel() == n and q_start.numel() == n + 1 and out.shape == q.shape):
+        raise ValueError("the arrays' lengths do not fit the table's requests and q")
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] != tokens:
+            raise ValueError("mask must be [tokens, words]")
+        words = mask.shape[1]
+    if lse is not None and not (_dtype_of(lse) == F32 and lse.is_contiguous() and lse.numel() == tokens * heads):
+        raise ValueError("lse must be a contiguous fp32 tensor [tokens, heads]")
+    _check(lib().colored_tree_attention(_h(ctx), cache, int(layer),
+                                        _rows(q, "q", heads, cache.head_dim, cache.dtype), heads,
+                                        _ints_of(q_start, "q_start"), tokens, int(max_nodes), blocks,
+                                        _ints_of(lens, "lens"), _ints_of(totals, "totals"),
+                                        _ints_of(mask, "mask", 8), words, scale, softcap,
+                                        _rows(out, "out", heads, cache.head_dim, cache.dtype), _addr(lse),
+                                        _addr(work), work.numel() * work.element_size(), _stream(stream)))
 
 
 class Bimodal:

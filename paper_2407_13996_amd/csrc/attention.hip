@@ -1,0 +1,867 @@
+// Attention of drafted tokens over the paged key/value cache.
+//
+// For one key/value head, the query rows of a request are its nodes' G =
+// n_heads / kv_heads query heads.  With S^T = K Q^T and O^T = V^T P^T a
+// query row is a column of both matrix products, that is, a lane (mod 16) of
+// every accumulator, so the softmax's running maximum and sum are one register
+// a row, and
+// rescaling, masking by node and the final division need no exchange between
+// lanes.  The products' operands come straight from the cache: 16 bytes of K
+// (8 dims of a token) or of V (8 tokens of a dim) are one lane's share of a
+// 16x16x32 MFMA operand.  S^T's accumulators hold four tokens of a row a lane;
+// two K tiles, whose rows are tokens 8 (r / 4) + r % 4 and those + 4, leave lane
+// group g with tokens 8g .. 8g + 7 of a 32-token step, in order: the P^T
+// operand.  No shuffle and no LDS between the two products.
+//
+// Split: every request's tokens are cut in steps of 32, and the steps of all
+// (request, block of rows, head) triples, "segments", form one line, which is
+// cut in kRanges equal ranges, one tile of the schedule each, whatever the
+// lengths: long and short requests fill the device alike.  A range's piece of a
+// segment that is not all of it leaves its maximum, sum and weighted V in
+// the workspace; a second launch joins them.  The cut depends on the lengths
+// only, so results do not depend on the CU mask.
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "kv_common.hpp"
+
+namespace sgdrc {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAttThreads = 256;
+constexpr int kAttWaves = kAttThreads / 64;
+constexpr uint32_t kStep = 32;            // tokens of a step of one wavefront
+constexpr uint32_t kRanges = 512;         // two workgroups on each of 256 CUs
+constexpr uint32_t kMinSteps = 4;         // steps of a range at least (one a wavefront)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttArgs {
+    KvView c;
+    RowsView q;
+    uint8_t *o;
+    uint64_t o_token, o_head;   // bytes
+    float *lse;
+    const uint32_t *q_start;
+    const uint32_t *table;
+    const int32_t *lens, *totals;
+    const uint64_t *mask;
+    float *work;
+    uint32_t n_requests, stride, n_tokens, max_nodes, mask_words;
+    uint32_t heads, group;      // query heads, query heads of a key/value head
+    float scale, softcap;
+};
+
+// A request as the kernels see it: device values brought into range.
+struct Req {
+    uint32_t start, nodes, total, ctx;
+    bool ok;
+};
+
+__device__ __forceinline__ Req load_req(const AttArgs &a, uint32_t r)
+{
+    Req q;
+    const uint32_t s = a.q_start[r], e = a.q_start[r + 1u];
+    const int32_t total = a.totals[r], ctx = a.lens[r];
+    const uint32_t cap = a.stride << a.c.bshift;
+    q.start = min(s, a.n_tokens);
+    const uint32_t end = max(min(e, a.n_tokens), q.start);
+    q.nodes = min(end - q.start, a.max_nodes);
+    q.total = total < 0 ? 0u : min((uint32_t)total, cap);
+    q.ctx = ctx < 0 ? 0u : min((uint32_t)ctx, q.total);
+    q.ok = s <= e && e <= a.n_tokens && e - s <= a.max_nodes && total >= 0 && (uint32_t)total <= cap && ctx >= 0 &&
+           ctx <= total;
+    return q;
+}
+
+// Steps of one segment of a request; a request whose cache is empty has one,
+// without tokens, which writes its rows.
+__device__ __forceinline__ uint32_t seg_steps(const Req &q)
+{
+    return max((q.total + kStep - 1u) / kStep, 1u);
+}
+
+__device__ __forceinline__ uint32_t row_blocks(const Req &q, uint32_t group, uint32_t rb)
+{
+    return (q.nodes * group + rb - 1u) / rb;
+}
+
+// All workgroups: s_line[r] = first step of request r in the line of steps,
+// s_line[n_requests] their number.
+__device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_t *s_line, uint32_t *s_sum,
+                                          uint32_t &err)
+{
+    const uint32_t R = a.n_requests;
+    const uint32_t per = (R + kAttThreads - 1u) / kAttThreads;
+    const uint32_t r0 = min(threadIdx.x * per, R), r1 = min(r0 + per, R);
+    uint32_t sum = 0u;
+    for (uint32_t r = r0; r < r1; ++r) {
+        const Req q = load_req(a, r);
+        err |= q.ok ? 0u : kDevErrSeq;
+        sum += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
+    }
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    uint32_t v = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_up(v, off, 64);
+        v += lane >= (uint32_t)off ? o : 0u;
+    }
+    if (lane == 63u)
+        s_sum[wave] = v;
+    __syncthreads();
+    uint32_t run = v - sum;
+    for (uint32_t w = 0; w < wave; ++w)
+        run += s_sum[w];
+    for (uint32_t r = r0; r < r1; ++r) {
+        const Req q = load_req(a, r);
+        s_line[r] = run;
+        run += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
+        if (r == R - 1u)
+            s_line[R] = run;
+    }
+    __syncthreads();
+}
+
+// The cut of a line of ``steps`` into ranges: range t is [cut(t), cut(t + 1)).
+__device__ __forceinline__ uint32_t n_ranges(uint32_t steps)
+{
+    return min(kRanges, (steps + kMinSteps - 1u) / kMinSteps);
+}
+
+__device__ __forceinline__ uint32_t range_cut(uint32_t t, uint32_t steps, uint32_t ranges)
+{
+    return (uint32_t)((uint64_t)t * steps / ranges);
+}
+
+// The range that step ``p`` is in.
+__device__ __forceinline__ uint32_t range_of(uint32_t p, uint32_t steps, uint32_t ranges)
+{
+    uint32_t t = (uint32_t)(((uint64_t)p * ranges) / steps);
+    while (t + 1u < ranges && range_cut(t + 1u, steps, ranges) <= p)
+        ++t;
+    return t;
+}
+
+// The last request that begins at or before step ``p`` and has any.
+__device__ __forceinline__ uint32_t find_request(const uint32_t *s_line, uint32_t R, uint32_t p)
+{
+    uint32_t lo = 0u, hi = R;
+    while (hi - lo > 1u) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (s_line[mid] <= p)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// A partial result in the workspace: per row {maximum, sum}, then the rows'
+// weighted V.  Range t has two: 2t for a piece that began in an earlier range,
+// 2t + 1 for one that goes on in the next.
+__device__ __forceinline__ float *part_stats(float *work, uint32_t part, uint32_t rb, uint32_t dim)
+{
+    return work + (uint64_t)part * rb * (dim + 2u);
+}
+
+__device__ __forceinline__ float *part_rows(float *work, uint32_t part, uint32_t rb, uint32_t dim)
+{
+    return part_stats(work, part, rb, dim) + rb * 2u;
+}
+
+template <int DT>
+__device__ __forceinline__ f32x4 att_mfma(u32x4 a, u32x4 b, f32x4 c)
+{
+    if (DT == SGDRC_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+}
+
+// Two fp32 values rounded to nearest even, side by side.
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float x, float y)
+{
+    const f32x2 v = {x, y};
+    if (DT == SGDRC_BF16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// Marks of infinities and NaN: 1 for +infinity, 64 for -infinity, 4096 for NaN
+// (a step has 32 tokens, so a sum of marks tells how many of each).
+template <int DT>
+constexpr uint32_t kOne = DT == SGDRC_BF16 ? 0x3F80u : 0x3C00u;
+
+// The marks of two elements of V, which become 0 where they have one.
+template <int DT>
+__device__ __forceinline__ uint32_t take_marks(uint32_t &x)
+{
+    constexpr uint32_t e = DT == SGDRC_BF16 ? 0x7F80u : 0x7C00u;
+    constexpr uint32_t m64 = DT == SGDRC_BF16 ? 0x4280u : 0x5400u, m4096 = DT == SGDRC_BF16 ? 0x4580u : 0x6C00u;
+    uint32_t marks = 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < 2u; ++i) {
+        const uint32_t v = (x >> (16u * i)) & 0xFFFFu;
+        if ((v & e) == e) {
+            marks |= ((v & 0x7FFFu) != e ? m4096 : v & 0x8000u ? m64 : kOne<DT>) << (16u * i);
+            x &= ~(0xFFFFu << (16u * i));
+        }
+    }
+    return marks;
+}
+
+// What a sum with these marks is: ``n`` of values with weights, ``n0`` of
+// values whose weight is 0 (0 times infinity).
+__device__ __forceinline__ float marked(float n, float n0)
+{
+    const uint32_t k = (uint32_t)n;
+    float v = k & 63u ? INFINITY : 0.0f;
+    v += (k >> 6) & 63u ? -INFINITY : 0.0f;
+    return k >> 12 || n0 != 0.0f ? NAN : v;
+}
+
+// The largest of a row's values over its four lanes.
+__device__ __forceinline__ float row_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+// n low bits, n of any size.
+__device__ __forceinline__ uint32_t low8(int32_t n)
+{
+    return n >= 8 ? 0xFFu : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
+// Which of the tokens ctx + j0 .. ctx + j0 + 7 node ``node`` sees, of ``drafted``.
+__device__ __forceinline__ uint32_t seen8(const AttArgs &a, uint32_t token, uint32_t node, int32_t j0,
+                                          int32_t drafted)
+{
+    uint32_t v;
+    if (!a.mask) {
+        v = low8((int32_t)node + 1 - j0);
+    } else {
+        const uint32_t lo = (uint32_t)max(j0, 0), w = lo >> 6, sh = lo & 63u;
+        const uint64_t *const row = a.mask + (uint64_t)token * a.mask_words;
+        uint64_t bits = w < a.mask_words ? row[w] >> sh : 0ull;
+        if (sh > 56u && w + 1u < a.mask_words)
+            bits |= row[w + 1u] << (64u - sh);
+        v = (uint32_t)bits & 0xFFu;
+        if (j0 < 0)
+            v = j0 <= -8 ? 0xFFu : (v << -j0) | low8(-j0);
+    }
+    return v & low8(drafted - j0);
+}
+
+template <int DT>
+__device__ __forceinline__ bool not_finite2(uint32_t x)
+{
+    constexpr uint32_t e = DT == SGDRC_BF16 ? 0x7F80u : 0x7C00u;
+    return (x & e) == e || ((x >> 16) & e) == e;
+}
+
+// D: head dimension.  NB: blocks of 16 query rows of a wavefront.  WQ: groups
+// of wavefronts with different rows (the other 4 / WQ share rows and take
+// every (4 / WQ)-th step).
+template <int DT, int D, int NB, int WQ>
+__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend(
+    AttArgs a, uint32_t n_tiles, Gate g)
+{
+    constexpr uint32_t WK = kAttWaves / WQ;
+    constexpr uint32_t kRows = 16u * NB * WQ;  // rows of a segment
+    constexpr int KK = D / 32;                 // MFMA steps along the head
+    constexpr int DD = D / 16;                 // blocks of 16 dims of O^T
+    // f16's P is scaled by 2^10: weights down to 2^-34 of the largest stay
+    // normal or subnormal numbers there (bf16 has fp32's range)
+    constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
+    __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
+    __shared__ uint32_t s_sum[kAttWaves];
+    __shared__ float s_ml[kAttWaves][16 * NB][2];
+    __shared__ __attribute__((aligned(16))) float s_o[kAttWaves][16][D + 4];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t col = lane & 15u, grp = lane >> 4;
+    const uint32_t wq = wave / WK, wk = wave % WK;
+    const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
+    uint32_t pro_err = 0u;
+    auto prologue = [&]() { plan_line(a, kRows, s_line, s_sum, pro_err); };
+    auto body = [&](uint32_t t, uint32_t &err) {
+        err |= pro_err;
+        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
+        const uint32_t ranges = n_ranges(steps);
+        const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
+        const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
+        for (uint32_t p = lo; p < hi;) {
+            const uint32_t r = __builtin_amdgcn_readfirstlane(find_request(s_line, a.n_requests, p));
+            const Req rq = load_req(a, r);
+            const uint32_t U = __builtin_amdgcn_readfirstlane(seg_steps(rq));
+            const uint32_t total = __builtin_amdgcn_readfirstlane(rq.total);
+            const uint32_t ctx = __builtin_amdgcn_readfirstlane(rq.ctx);
+            const uint32_t rows = __builtin_amdgcn_readfirstlane(rq.nodes * a.group);
+            const uint32_t start = __builtin_amdgcn_readfirstlane(rq.start);
+            const uint32_t blocks = (rows + kRows - 1u) / kRows;
+            const uint32_t at = p - __builtin_amdgcn_readfirstlane(s_line[r]);
+            const uint32_t seg = at / U, u0 = at % U;
+            const uint32_t h = seg / blocks, row0 = seg % blocks * kRows;
+            const uint32_t u1 = min(U, u0 + (hi - p));
+            const bool first = p == lo;
+            p += u1 - u0;
+
+            // this wavefront's rows of Q: column ``col`` of block b is row
+            // row0 + 16 (wq NB + b) + col, node row / group
+            u32x4 qf[NB][KK];
+            uint32_t tok[NB], node[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t row = min(row0 + 16u * (wq * NB + b) + col, rows - 1u);
+                node[b] = row / a.group;
+                tok[b] = start + node[b];
+                const uint8_t *const qp = a.q.ptr + tok[b] * a.q.token + (h * a.group + row % a.group) * a.q.head;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    qf[b][kk] = *reinterpret_cast<const u32x4 *>(qp + (kk * 4u + grp) * 16u);
+            }
+            f32x4 acc[NB][DD];
+            float m[NB], l[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                m[b] = -INFINITY;
+                l[b] = 0.0f;
+#pragma unroll
+                for (int dd = 0; dd < DD; ++dd)
+                    acc[b][dd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            const uint32_t *const row_table = a.table + (uint64_t)r * a.stride;
+            const uint32_t last_block = total ? (total - 1u) >> a.c.bshift : 0u;
+            // K's lanes: token 8 (col / 4) + col % 4 (+ 4) of the step
+            const uint32_t k_tok = (col >> 2) * 8u + (col & 3u);
+            const uint8_t *const head = a.c.pool + h * head_bytes<D>(a.c.bshift);
+            const uint32_t bmask = (1u << a.c.bshift) - 1u;
+
+            for (uint32_t u = u0 + wk; u < u1; u += WK) {
+                const uint32_t base = u * kStep;
+                // a block holds whole groups of 8 tokens; pages past the cache's
+                // end are not looked up (their entries may hold anything)
+                uint32_t bad = 0u, bad_k = 0u;
+                const uint32_t ke = checked_page(row_table, min((base + (col >> 2) * 8u) >> a.c.bshift, last_block),
+                                                 a.c.pool_pages, bad_k);
+                const uint32_t ve = checked_page(row_table, min((base + grp * 8u) >> a.c.bshift, last_block),
+                                                 a.c.pool_pages, bad);
+                if (total == 0u)
+                    bad = bad_k = 1u;
+                else
+                    err |= bad;
+                const uint8_t *const kp = head + ((uint64_t)(bad_k ? 0u : ke) << a.c.shift);
+                const uint8_t *const vp = head + ((uint64_t)(bad ? 0u : ve) << a.c.shift);
+                const uint32_t kt = (base + k_tok) & bmask, vt = ((base + grp * 8u) & bmask) >> 3;
+                u32x4 kf[2][KK], vf[DD];
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    kf[0][kk] = *reinterpret_cast<const u32x4 *>(kp + k_off<D>(kk * 4u + grp, kt, a.c.bshift));
+                    kf[1][kk] = *reinterpret_cast<const u32x4 *>(kp + k_off<D>(kk * 4u + grp, kt + 4u, a.c.bshift));
+                }
+#pragma unroll
+                for (int dd = 0; dd < DD; ++dd)
+                    vf[dd] = *reinterpret_cast<const u32x4 *>(vp + v_off<D>(vt, dd * 16u + col, a.c.bshift));
+
+                f32x4 s[NB][2];
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        s[b][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int kk = 0; kk < KK; ++kk)
+                            s[b][x] = att_mfma<DT>(kf[x][kk], qf[b][kk], s[b][x]);
+                    }
+                if (a.softcap > 0.0f) {
+                    // cap tanh(s scale / cap) in units of log 2; tanh y = 1 - 2 / (1 + e^2y)
+                    const float in = a.scale / a.softcap * 2.0f * kLog2e, out = a.softcap * kLog2e;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float e = __builtin_amdgcn_exp2f(s[b][x][i] * in);
+                                s[b][x][i] = out - 2.0f * out * __builtin_amdgcn_rcpf(1.0f + e);
+                            }
+                }
+                const int32_t j0 = (int32_t)(base + grp * 8u) - (int32_t)ctx;
+                const int32_t drafted = (int32_t)total - (int32_t)ctx;
+                const bool edge = base + kStep > ctx || __ballot(bad != 0u) != 0ull;
+                uint32_t seen[NB];
+                bool odd = false;  // a value that must not meet a weight of zero
+                if (edge) {
+                    const uint32_t there = bad ? 0u : low8(drafted - j0);
+#pragma unroll
+                    for (int dd = 0; dd < DD; ++dd)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t two = (there >> (2 * w)) & 3u;
+                            vf[dd][w] &= (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
+                            odd = odd || not_finite2<DT>(vf[dd][w]);
+                        }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        seen[b] = seen8(a, tok[b], node[b], j0, drafted) & there;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                s[b][x][i] = (seen[b] >> (4 * x + i)) & 1u ? s[b][x][i] : -INFINITY;
+                    }
+                }
+                u32x4 pf[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    float mx = s[b][0][0];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            mx = fmaxf(mx, s[b][x][i]);
+                    mx = row_max(mx);
+                    if (__ballot(mx > m[b]) != 0ull) {
+                        const float mn = fmaxf(m[b], mx);
+                        const float use = mn == -INFINITY ? 0.0f : mn;
+                        const float f = __builtin_amdgcn_exp2f((m[b] - use) * c2);
+                        m[b] = mn;
+                        l[b] *= f;
+#pragma unroll
+                        for (int dd = 0; dd < DD; ++dd)
+                            acc[b][dd] *= f;
+                    }
+                    const float sub = (m[b] == -INFINITY ? 0.0f : m[b] * c2) - kLift;
+                    float pv[8];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float e = __builtin_amdgcn_exp2f(s[b][x][i] * c2 - sub);
+                            pv[4 * x + i] = e;
+                            l[b] += e;
+                        }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        pf[b][w] = pack2<DT>(pv[2 * w], pv[2 * w + 1]);
+                }
+                if (edge && __ballot(odd) != 0ull) {
+                    // infinities or NaN among the drafted values must not meet the
+                    // weight 0 of a row that does not see them.  They are taken
+                    // out of V, and a product of marks counts those that each row
+                    // sees: such a sum is infinite or NaN, whatever the rest is
+                    u32x4 some[NB], none[NB];
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (uint32_t w = 0; w < 4u; ++w) {
+                            some[b][w] = none[b][w] = 0u;
+#pragma unroll
+                            for (uint32_t i = 0; i < 2u; ++i)
+                                if ((seen[b] >> (2u * w + i)) & 1u) {
+                                    const bool zero = ((pf[b][w] >> (16u * i)) & 0xFFFFu) == 0u;
+                                    some[b][w] |= zero ? 0u : kOne<DT> << (16u * i);
+                                    none[b][w] |= zero ? kOne<DT> << (16u * i) : 0u;
+                                }
+                        }
+#pragma unroll
+                    for (int dd = 0; dd < DD; ++dd) {
+                        u32x4 marks;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            uint32_t two = vf[dd][w];
+                            marks[w] = take_marks<DT>(two);
+                            vf[dd][w] = two;
+                        }
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) {
+                            const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+                            acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], acc[b][dd]);
+                            const f32x4 n = att_mfma<DT>(marks, some[b], z), n0 = att_mfma<DT>(marks, none[b], z);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                acc[b][dd][i] += marked(n[i], n0[i]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);  // one block's marks at a time
+                    }
+                } else {
+#pragma unroll
+                    for (int dd = 0; dd < DD; ++dd)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], acc[b][dd]);
+                }
+            }
+
+            // Join the wavefronts that shared the rows: maxima and sums first,
+            // then the weighted V, 16 rows at a time.
+            float f[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                l[b] = row_sum(l[b]);
+                if (grp == 0u) {
+                    s_ml[wave][16 * b + col][0] = m[b];
+                    s_ml[wave][16 * b + col][1] = l[b];
+                }
+            }
+            __syncthreads();
+            const bool whole = u0 == 0u && u1 == U;
+            const uint32_t part = 2u * t + (first && u0 != 0u ? 0u : 1u);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float mj = -INFINITY;
+#pragma unroll
+                for (uint32_t w = 0; w < WK; ++w)
+                    mj = fmaxf(mj, s_ml[wq * WK + w][16 * b + col][0]);
+                const float use = mj == -INFINITY ? 0.0f : mj;
+                float lj = 0.0f;
+#pragma unroll
+                for (uint32_t w = 0; w < WK; ++w)
+                    lj += s_ml[wq * WK + w][16 * b + col][1] *
+                          __builtin_amdgcn_exp2f((s_ml[wq * WK + w][16 * b + col][0] - use) * c2);
+                f[b] = __builtin_amdgcn_exp2f((m[b] - use) * c2);
+                if (whole)
+                    f[b] = lj > 0.0f ? f[b] / lj : lj == 0.0f ? 0.0f : lj;  // NaN stays NaN
+                const uint32_t in = 16u * (wq * NB + b) + col;
+                if (wk == 0u && grp == 0u && row0 + in < rows) {
+                    if (!whole) {
+                        float *const st = part_stats(a.work, part, kRows, D) + in * 2u;
+                        st[0] = mj;
+                        st[1] = lj;
+                    } else if (a.lse) {
+                        a.lse[(uint64_t)tok[b] * a.heads + h * a.group + (row0 + in) % a.group] =
+                            lj == 0.0f ? -INFINITY : (mj * c2 - kLift + __log2f(lj)) * kLn2;
+                    }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int dd = 0; dd < DD; ++dd)
+                    *reinterpret_cast<f32x4 *>(&s_o[wave][col][dd * 16 + grp * 4u]) = acc[b][dd] * f[b];
+                __syncthreads();
+                // each group of WK wavefronts adds up its own 16 rows, 4 dims a thread
+                for (uint32_t i = threadIdx.x % (64u * WK); i < 16u * (D / 4); i += 64u * WK) {
+                    const uint32_t x = i / (D / 4), d = i % (D / 4) * 4u;
+                    const uint32_t in = 16u * (wq * NB + b) + x, row = row0 + in;
+                    f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[wq * WK][x][d]);
+#pragma unroll
+                    for (uint32_t w = 1; w < WK; ++w)
+                        v += *reinterpret_cast<const f32x4 *>(&s_o[wq * WK + w][x][d]);
+                    if (row < rows) {
+                        if (whole) {
+                            uint8_t *const op = a.o + (start + row / a.group) * a.o_token +
+                                                (h * a.group + row % a.group) * a.o_head + d * 2u;
+                            const u32x2 two = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+                            *reinterpret_cast<u32x2 *>(op) = two;
+                        } else {
+                            *reinterpret_cast<f32x4 *>(part_rows(a.work, part, kRows, D) + (uint64_t)in * D + d) = v;
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+        }
+    };
+    single_tile_loop(g, n_tiles, prologue, body);
+}
+
+constexpr uint32_t kJoinRows = 4;  // rows of a join tile, one a wavefront
+
+// Joins the pieces of segments that lie in several ranges, a wavefront a row
+// (token and query head).  Segments inside one range were written whole.
+template <int DT, int D>
+__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t rb, uint32_t n_tiles, Gate g)
+{
+    constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
+    constexpr uint32_t PER = (D + 63) / 64;
+    __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
+    __shared__ uint32_t s_sum[kAttWaves];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63u;
+    const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
+    uint32_t pro_err = 0u;
+    auto prologue = [&]() { plan_line(a, rb, s_line, s_sum, pro_err); };
+    auto body = [&](uint32_t t, uint32_t &) {
+        const uint64_t i = (uint64_t)t * kJoinRows + wave;
+        const uint32_t token = (uint32_t)(i / a.heads), qh = (uint32_t)(i % a.heads);
+        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
+        // the last request whose rows begin at or before the token
+        uint32_t rlo = 0u, rhi = a.n_requests;
+        while (rhi - rlo > 1u) {
+            const uint32_t mid = (rlo + rhi) >> 1;
+            if (a.q_start[mid] <= token)
+                rlo = mid;
+            else
+                rhi = mid;
+        }
+        const uint32_t r = __builtin_amdgcn_readfirstlane(rlo);
+        const Req rq = load_req(a, r);
+        const bool mine = token < a.n_tokens && token >= rq.start && token - rq.start < rq.nodes && steps != 0u;
+        const uint32_t node = token - rq.start;
+        const uint32_t ranges = n_ranges(steps);
+        uint32_t t0 = 0u, t1 = 0u, in = 0u, seg0 = 0u;
+        if (mine) {
+            const uint32_t row = node * a.group + qh % a.group;
+            const uint32_t U = seg_steps(rq), blocks = row_blocks(rq, a.group, rb);
+            seg0 = s_line[r] + (qh / a.group * blocks + row / rb) * U;
+            in = row % rb;
+            t0 = range_of(seg0, steps, ranges);
+            t1 = range_of(seg0 + U - 1u, steps, ranges);
+        }
+        if (t0 < t1) {
+            // a segment's first piece is its range's last, the others their range's first
+            float mx = -INFINITY;
+            for (uint32_t q = t0 + lane; q <= t1; q += 64u)
+                mx = fmaxf(mx, part_stats(a.work, 2u * q + (q == t0 ? 1u : 0u), rb, D)[in * 2u]);
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1)
+                mx = fmaxf(mx, __shfl_xor(mx, off, 64));
+            const float use = mx == -INFINITY ? 0.0f : mx;
+            float l = 0.0f, v[PER];
+#pragma unroll
+            for (uint32_t e = 0; e < PER; ++e)
+                v[e] = 0.0f;
+            for (uint32_t q0 = t0; q0 <= t1; q0 += 64u) {
+                const uint32_t q = q0 + lane;
+                float f = 0.0f;
+                if (q <= t1) {
+                    const float *const st = part_stats(a.work, 2u * q + (q == t0 ? 1u : 0u), rb, D) + in * 2u;
+                    f = __builtin_amdgcn_exp2f((st[0] - use) * c2);
+                    l += st[1] * f;
+                }
+                const uint32_t n = min(t1 + 1u - q0, 64u);
+                for (uint32_t k = 0; k < n; ++k) {
+                    const uint32_t qq = q0 + k;
+                    const float w = __shfl(f, (int)k, 64);
+                    const float *const src = part_rows(a.work, 2u * qq + (qq == t0 ? 1u : 0u), rb, D) + (uint64_t)in * D;
+#pragma unroll
+                    for (uint32_t e = 0; e < PER; ++e)
+                        if (lane + 64u * e < (uint32_t)D)
+                            v[e] += src[lane + 64u * e] * w;
+                }
+            }
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1)
+                l += __shfl_xor(l, off, 64);
+            const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+            uint8_t *const op = a.o + token * a.o_token + qh * a.o_head;
+#pragma unroll
+            for (uint32_t e = 0; e < PER; ++e)
+                if (lane + 64u * e < (uint32_t)D)
+                    *reinterpret_cast<uint16_t *>(op + (lane + 64u * e) * 2u) = (uint16_t)pack2<DT>(v[e] * inv, 0.0f);
+            if (a.lse && lane == 0u)
+                a.lse[(uint64_t)token * a.heads + qh] =
+                    l == 0.0f ? -INFINITY : (mx * c2 - kLift + __log2f(l)) * kLn2;
+        }
+    };
+    single_tile_loop(g, n_tiles, prologue, body);
+}
+
+// -------------------------------------------------------------------- host
+
+typedef void (*AttKernel)(AttArgs, uint32_t, Gate);
+typedef void (*JoinKernel)(AttArgs, uint32_t, uint32_t, Gate);
+
+// How a call's rows are spread: rows = 16 nb wq of a segment.
+struct AttForm {
+    uint32_t nb, wq;
+};
+
+static AttForm att_form(uint32_t dim, uint32_t rows)
+{
+    if (rows <= 16u)
+        return {1, 1};
+    if (rows <= 32u)
+        return {2, 1};
+    if (dim == 256u)  // four blocks of rows would not fit the registers
+        return rows <= 64u ? AttForm{2, 2} : AttForm{2, 4};
+    if (rows <= 64u)
+        return {4, 1};
+    return rows <= 128u ? AttForm{4, 2} : AttForm{4, 4};
+}
+
+template <int DT, int D>
+static AttKernel att_kernel_d(AttForm f)
+{
+    if (f.nb == 1)
+        return k_attend<DT, D, 1, 1>;
+    if (f.nb == 2 && f.wq == 1)
+        return k_attend<DT, D, 2, 1>;
+    if constexpr (D == 256) {
+        return f.wq == 2 ? k_attend<DT, D, 2, 2> : k_attend<DT, D, 2, 4>;
+    } else {
+        if (f.wq == 1)
+            return k_attend<DT, D, 4, 1>;
+        return f.wq == 2 ? k_attend<DT, D, 4, 2> : k_attend<DT, D, 4, 4>;
+    }
+}
+
+template <int DT>
+static AttKernel att_kernel(uint32_t dim, AttForm f, JoinKernel *join)
+{
+    switch (dim) {
+    case 64: *join = k_attend_join<DT, 64>; return att_kernel_d<DT, 64>(f);
+    case 96: *join = k_attend_join<DT, 96>; return att_kernel_d<DT, 96>(f);
+    case 128: *join = k_attend_join<DT, 128>; return att_kernel_d<DT, 128>(f);
+    default: *join = k_attend_join<DT, 256>; return att_kernel_d<DT, 256>(f);
+    }
+}
+
+template <typename K>
+static int att_occupancy(K k)
+{
+    static std::mutex mu;
+    static std::unordered_map<const void *, int> cache;
+    std::lock_guard<std::mutex> lock(mu);
+    auto it = cache.find((const void *)k);
+    if (it != cache.end())
+        return it->second;
+    const int n = occupancy(k, kAttThreads);
+    cache[(const void *)k] = n;
+    return n;
+}
+
+static int check_att_shape(const sgdrc_kv_cache *cache, uint32_t n_heads, uint32_t max_nodes)
+{
+    const int rc = check_kv_cache(cache);
+    if (rc)
+        return rc;
+    if (n_heads == 0 || n_heads > SGDRC_MAX_HEADS || n_heads % cache->kv_heads)
+        return set_error(SGDRC_EINVAL, "n_heads %u: above %d or not a multiple of %u key/value heads", n_heads,
+                         SGDRC_MAX_HEADS, cache->kv_heads);
+    if (max_nodes < 1 || max_nodes > SGDRC_MAX_NODES)
+        return set_error(SGDRC_EINVAL, "max_nodes %u outside 1..%d", max_nodes, SGDRC_MAX_NODES);
+    return SGDRC_OK;
+}
+
+static uint64_t att_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads, uint32_t max_nodes)
+{
+    const AttForm f = att_form(cache->head_dim, max_nodes * (n_heads / cache->kv_heads));
+    return 2ull * kRanges * 16u * f.nb * f.wq * (cache->head_dim + 2u) * sizeof(float);
+}
+
+}  // namespace sgdrc
+
+using namespace sgdrc;
+
+extern "C" {
+
+int sgdrc_tree_attention_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads, uint32_t max_nodes, uint64_t *bytes)
+{
+    clear_error();
+    if (!bytes)
+        return set_error(SGDRC_EINVAL, "bytes is NULL");
+    const int rc = check_att_shape(cache, n_heads, max_nodes);
+    if (rc)
+        return rc;
+    *bytes = att_workspace(cache, n_heads, max_nodes);
+    return SGDRC_OK;
+}
+
+int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer, const sgdrc_rows *q,
+                           uint32_t n_heads, const uint32_t *d_q_start, uint32_t n_tokens, uint32_t max_nodes,
+                           const sgdrc_kv_blocks *blocks, const int32_t *d_lens, const int32_t *d_totals,
+                           const uint64_t *d_mask, uint32_t mask_words, float scale, float softcap,
+                           const sgdrc_rows *o, float *d_lse, void *d_work, uint64_t work_bytes, void *stream)
+{
+    clear_error();
+    int rc = check_att_shape(cache, n_heads, max_nodes);
+    if (rc || (rc = check_kv_blocks(blocks, cache->block_tokens)))
+        return rc;
+    if (layer >= cache->n_layers)
+        return set_error(SGDRC_EINVAL, "layer %u of %u", layer, cache->n_layers);
+    if (d_mask && (mask_words < 1 || mask_words > SGDRC_MAX_NODES / 64))
+        return set_error(SGDRC_EINVAL, "mask_words %u outside 1..%d", mask_words, SGDRC_MAX_NODES / 64);
+    if (!(scale > 0.0f) || !std::isfinite(scale))
+        return set_error(SGDRC_EINVAL, "scale is not positive and finite");
+    if (!(softcap >= 0.0f) || !std::isfinite(softcap))
+        return set_error(SGDRC_EINVAL, "softcap is negative or not finite");
+    if ((rc = check_aligned(d_q_start, 4, "q_start")) || (rc = check_aligned(d_lens, 4, "lens")) ||
+        (rc = check_aligned(d_totals, 4, "totals")) || (rc = check_aligned(d_work, 256, "work")) ||
+        (d_mask && (rc = check_aligned(d_mask, 8, "mask"))) || (d_lse && (rc = check_aligned(d_lse, 4, "lse"))))
+        return rc;
+    if (work_bytes < att_workspace(cache, n_heads, max_nodes))
+        return set_error(SGDRC_EINVAL, "workspace of %llu bytes, %llu are needed", (unsigned long long)work_bytes,
+                         (unsigned long long)att_workspace(cache, n_heads, max_nodes));
+    if (n_tokens > 0x7FFFFFFFu)
+        return set_error(SGDRC_EINVAL, "n_tokens above 2^31 - 1");
+    const uint32_t group = n_heads / cache->kv_heads;
+    const AttForm f = att_form(cache->head_dim, max_nodes * group);
+    const uint32_t rb = 16u * f.nb * f.wq;
+    const uint64_t seg = ((uint64_t)blocks->stride * cache->block_tokens + kStep - 1u) / kStep;
+    const uint64_t blocks_of_rows = (max_nodes * group + rb - 1u) / rb;
+    if (seg * blocks_of_rows * cache->kv_heads > (1ull << 31) / blocks->n_requests)
+        return set_error(SGDRC_EINVAL, "more than 2^31 steps of %u tokens at full tables", kStep);
+    const uint64_t join_tiles = ((uint64_t)n_tokens * n_heads + kJoinRows - 1u) / kJoinRows;
+    if (join_tiles >= (1ull << 31) - 65536u)
+        return set_error(SGDRC_EINVAL, "too many tokens");
+    if (n_tokens && ((rc = check_rows(q, "q")) || (rc = check_rows(o, "o"))))
+        return rc;
+    Ctx *c = nullptr;
+    if ((rc = check_ctx(ctx, &c)))
+        return rc;
+    if (n_tokens == 0)
+        return SGDRC_OK;
+
+    AttArgs a;
+    a.c = kv_view(cache, layer);
+    a.q = rows_view(q);
+    a.o = static_cast<uint8_t *>(o->ptr);
+    a.o_token = o->token_stride * 2u;
+    a.o_head = o->head_stride * 2u;
+    a.lse = d_lse;
+    a.q_start = d_q_start;
+    a.table = blocks->table;
+    a.lens = d_lens;
+    a.totals = d_totals;
+    a.mask = d_mask;
+    a.work = static_cast<float *>(d_work);
+    a.n_requests = blocks->n_requests;
+    a.stride = blocks->stride;
+    a.n_tokens = n_tokens;
+    a.max_nodes = max_nodes;
+    a.mask_words = mask_words;
+    a.heads = n_heads;
+    a.group = group;
+    a.scale = scale;
+    a.softcap = softcap;
+    JoinKernel join = nullptr;
+    const AttKernel k = cache->dtype == SGDRC_BF16 ? att_kernel<SGDRC_BF16>(cache->head_dim, f, &join)
+                                                   : att_kernel<SGDRC_F16>(cache->head_dim, f, &join);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    Gate g;
+    LaunchInfo li;
+    if ((rc = make_gate(c, stream, kRanges, kStreamGroupCus, &g, &li, false, true)))
+        return rc;
+    hipLaunchKernelGGL(k, dim3(gated_grid(c, att_occupancy(k), kRanges, li)), dim3(kAttThreads), 0, s, a, kRanges, g);
+    SGDRC_HIP(hipGetLastError());
+    if ((rc = finish_static_tlog(g, s)))
+        return rc;
+    if ((rc = make_gate(c, stream, join_tiles, kStreamGroupCus, &g, &li, false, true)))
+        return rc;
+    hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join), join_tiles, li)), dim3(kAttThreads), 0, s, a, rb,
+                       (uint32_t)join_tiles, g);
+    SGDRC_HIP(hipGetLastError());
+    return finish_static_tlog(g, s);
+}
+
+}  // extern "C"

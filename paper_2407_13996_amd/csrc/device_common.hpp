@@ -23,6 +23,7 @@ constexpr uint32_t kDevErrPtRange = 1u;
 constexpr uint32_t kDevFlagGateFallback = 2u;
 constexpr uint32_t kDevErrSuspendedDropped = 4u;  // a suspended launch was discarded unresumed
 constexpr uint32_t kDevErrHandBack = 8u;          // a handed-back tile index out of range
+constexpr uint32_t kDevErrSeq = 16u;              // a length, row start, slot or path out of range
 
 // Queue slot states (QueueSlot::state).
 constexpr uint32_t kSlotIdle = 0u;
@@ -704,6 +705,73 @@ __device__ __forceinline__ void tile_loop(const Gate &g, uint32_t n_tiles, Prolo
         static_tile_loop(g, n_tiles, prologue, body);
     else
         gated_tile_loop<CL>(g, n_tiles, prologue, body, NoOp(), NoOp());
+}
+
+// The gate's two schedules with one call of ``body``, for bodies so large that
+// a copy per schedule would cost registers and code: under a static schedule
+// as static_tile_loop, otherwise tickets of one queue for the whole device
+// (the host asks for a gate without queue groups), and the tiles left if no
+// workgroup reached an allowed CU to the last workgroup of the grid (flagged).
+// ``prologue`` and ``body(tile, err)`` as in gated_tile_loop; every thread of
+// the workgroup runs the same iterations.
+template <typename Prologue, typename Body>
+__device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles, Prologue prologue, Body body)
+{
+    __shared__ uint32_t s_ticket;
+    __shared__ uint32_t s_flag;
+    uint32_t xcc;
+    asm volatile("s_getreg_b32 %0, hwreg(HW_REG_XCC_ID)" : "=s"(xcc));
+    const uint32_t a = g.xcd_rank[xcc & 0xFu];
+    const uint32_t cu = !g.statics || g.log_cu ? (my_cu_entry(g) & 0xFFFFu) : (uint32_t)kMaxCus;
+    prologue();
+    if (g.tlog && blockIdx.x == 0 && threadIdx.x == 0)
+        __hip_atomic_store(&g.tlog[0], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    uint32_t err = 0u;
+    // where the next tile comes from: the static stride, the queue, what is left
+    enum { kStride, kQueue, kLeft };
+    uint32_t from = g.statics ? kStride : kQueue;
+    const uint32_t workers = (gridDim.x / g.n_xcd) * g.n_allowed_xcd;
+    uint32_t t = a != 0xFFu ? (blockIdx.x / g.n_xcd) * g.n_allowed_xcd + a : n_tiles;
+    t = __builtin_amdgcn_readfirstlane(t);
+    const bool allowed = __builtin_amdgcn_readfirstlane(cu_allowed(g, cu) ? 1u : 0u) != 0u;
+    for (;;) {
+        uint32_t tile = n_tiles;
+        if (from == kQueue) {
+            if (allowed)
+                tile = claim_ticket(&g.q->grp_next[0], &s_ticket);
+            if (tile >= n_tiles) {
+                if (!arrive_last(g, &s_flag))
+                    break;
+                t = __builtin_amdgcn_readfirstlane(
+                    __hip_atomic_load(&g.q->grp_next[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+                if (t < n_tiles)
+                    err |= threadIdx.x == 0 ? kDevFlagGateFallback : 0u;
+                from = kLeft;
+            }
+        }
+        if (from != kQueue) {
+            tile = t;
+            if (tile >= n_tiles)
+                break;
+            t += from == kStride ? workers : 1u;
+        }
+        log_tile(g, cu, tile);
+        body(tile, err);
+    }
+    if (from == kLeft) {
+        reset_slot(g.q);
+        if (g.tlog && threadIdx.x == 0) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __hip_atomic_store(&g.tlog[1], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (from == kStride)
+        static_end(g, a, NoOp(), err);
+    else if (err != 0u)
+        raise_flag(g.err, err);
 }
 
 // Wavefront-granular form of gated_tile_loop, for bodies whose work is
