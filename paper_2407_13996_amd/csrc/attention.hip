@@ -36,9 +36,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttThreads = 256;
 constexpr int kAttWaves = kAttThreads / 64;
-constexpr uint32_t kStep = 32;            // tokens of a step of one wavefront
-constexpr uint32_t kRanges = 512;         // two workgroups on each of 256 CUs
-constexpr uint32_t kMinSteps = 4;         // steps of a range at least (one a wavefront)
+constexpr uint32_t kStep = 32;            // tokens of a step
+constexpr uint32_t kMinSteps = 4;         // steps of a range at least
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -55,6 +54,7 @@ struct AttArgs {
     float *work;
     uint32_t n_requests, stride, n_tokens, max_nodes, mask_words;
     uint32_t heads, group;      // query heads, query heads of a key/value head
+    uint32_t most_ranges;       // pieces that the line of steps is cut in at most
     float scale, softcap;
 };
 
@@ -94,11 +94,12 @@ __device__ __forceinline__ uint32_t row_blocks(const Req &q, uint32_t group, uin
 
 // All workgroups: s_line[r] = first step of request r in the line of steps,
 // s_line[n_requests] their number.
+template <uint32_t THREADS>
 __device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_t *s_line, uint32_t *s_sum,
                                           uint32_t &err)
 {
     const uint32_t R = a.n_requests;
-    const uint32_t per = (R + kAttThreads - 1u) / kAttThreads;
+    const uint32_t per = (R + THREADS - 1u) / THREADS;
     const uint32_t r0 = min(threadIdx.x * per, R), r1 = min(r0 + per, R);
     uint32_t sum = 0u;
     for (uint32_t r = r0; r < r1; ++r) {
@@ -130,9 +131,9 @@ __device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_
 }
 
 // The cut of a line of ``steps`` into ranges: range t is [cut(t), cut(t + 1)).
-__device__ __forceinline__ uint32_t n_ranges(uint32_t steps)
+__device__ __forceinline__ uint32_t n_ranges(const AttArgs &a, uint32_t steps)
 {
-    return min(kRanges, (steps + kMinSteps - 1u) / kMinSteps);
+    return min(a.most_ranges, (steps + kMinSteps - 1u) / kMinSteps);
 }
 
 __device__ __forceinline__ uint32_t range_cut(uint32_t t, uint32_t steps, uint32_t ranges)
@@ -198,27 +199,45 @@ __device__ __forceinline__ uint32_t pack2(float x, float y)
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
 
+// Two 16-bit elements at a time, without comparisons (their results would
+// take scalar registers, of which a step in this state has none left).
+// All of a half's bits where its top bit is set in ``x``.
+__device__ __forceinline__ uint32_t spread_top(uint32_t x)
+{
+    return ((x >> 15) & 0x00010001u) * 0xFFFFu;
+}
+
+// Halves that hold more than ``least`` - 1 without their sign, by their top bits.
+template <uint32_t LEAST>
+__device__ __forceinline__ uint32_t top_from(uint32_t x)
+{
+    return ((x & 0x7FFF7FFFu) + (0x8000u - LEAST) * 0x00010001u) & 0x80008000u;
+}
+
+template <int DT>
+constexpr uint32_t kInf = DT == SGDRC_BF16 ? 0x7F80u : 0x7C00u;
+
+// The halves' masks of tokens 2 w and 2 w + 1 in ``bits``.
+__device__ __forceinline__ uint32_t pair_mask(uint32_t bits, int w)
+{
+    return spread_top((((bits >> (2 * w)) & 1u) << 15) | (((bits >> (2 * w + 1)) & 1u) << 31));
+}
+
 // Marks of infinities and NaN: 1 for +infinity, 64 for -infinity, 4096 for NaN
 // (a step has 32 tokens, so a sum of marks tells how many of each).
 template <int DT>
-constexpr uint32_t kOne = DT == SGDRC_BF16 ? 0x3F80u : 0x3C00u;
+constexpr uint32_t kOne = (DT == SGDRC_BF16 ? 0x3F80u : 0x3C00u) * 0x00010001u;
 
 // The marks of two elements of V, which become 0 where they have one.
 template <int DT>
 __device__ __forceinline__ uint32_t take_marks(uint32_t &x)
 {
-    constexpr uint32_t e = DT == SGDRC_BF16 ? 0x7F80u : 0x7C00u;
-    constexpr uint32_t m64 = DT == SGDRC_BF16 ? 0x4280u : 0x5400u, m4096 = DT == SGDRC_BF16 ? 0x4580u : 0x6C00u;
-    uint32_t marks = 0u;
-#pragma unroll
-    for (uint32_t i = 0; i < 2u; ++i) {
-        const uint32_t v = (x >> (16u * i)) & 0xFFFFu;
-        if ((v & e) == e) {
-            marks |= ((v & 0x7FFFu) != e ? m4096 : v & 0x8000u ? m64 : kOne<DT>) << (16u * i);
-            x &= ~(0xFFFFu << (16u * i));
-        }
-    }
-    return marks;
+    constexpr uint32_t m64 = (DT == SGDRC_BF16 ? 0x4280u : 0x5400u) * 0x00010001u;
+    constexpr uint32_t m4096 = (DT == SGDRC_BF16 ? 0x4580u : 0x6C00u) * 0x00010001u;
+    const uint32_t off = spread_top(top_from<kInf<DT>>(x)), nan = spread_top(top_from<kInf<DT> + 1u>(x));
+    const uint32_t neg = spread_top(x);
+    x &= ~off;
+    return off & ((nan & m4096) | (~nan & ((neg & m64) | (~neg & kOne<DT>))));
 }
 
 // What a sum with these marks is: ``n`` of values with weights, ``n0`` of
@@ -270,27 +289,322 @@ __device__ __forceinline__ uint32_t seen8(const AttArgs &a, uint32_t token, uint
     return v & low8(drafted - j0);
 }
 
-template <int DT>
-__device__ __forceinline__ bool not_finite2(uint32_t x)
+// A range's part of one segment.
+struct Piece {
+    uint32_t r, h;              // request, key/value head
+    uint32_t start, rows, row0; // the request's first token, its rows; the segment's first row
+    uint32_t total, ctx;
+    uint32_t u0, u1;            // steps
+    uint32_t part;              // its place in the workspace
+    bool whole;                 // all of the segment
+};
+
+// The piece that begins at step ``p`` of the line, in range ``t`` = [lo, hi); all values uniform.
+__device__ __forceinline__ Piece take_piece(const AttArgs &a, const uint32_t *s_line, uint32_t rb, uint32_t t,
+                                            uint32_t lo, uint32_t hi, uint32_t p)
 {
-    constexpr uint32_t e = DT == SGDRC_BF16 ? 0x7F80u : 0x7C00u;
-    return (x & e) == e || ((x >> 16) & e) == e;
+    Piece x;
+    x.r = __builtin_amdgcn_readfirstlane(find_request(s_line, a.n_requests, p));
+    const Req rq = load_req(a, x.r);
+    const uint32_t U = __builtin_amdgcn_readfirstlane(seg_steps(rq));
+    x.total = __builtin_amdgcn_readfirstlane(rq.total);
+    x.ctx = __builtin_amdgcn_readfirstlane(rq.ctx);
+    x.rows = __builtin_amdgcn_readfirstlane(rq.nodes * a.group);
+    x.start = __builtin_amdgcn_readfirstlane(rq.start);
+    const uint32_t blocks = (x.rows + rb - 1u) / rb;
+    const uint32_t at = p - __builtin_amdgcn_readfirstlane(s_line[x.r]);
+    const uint32_t seg = at / U;
+    x.u0 = at % U;
+    x.u1 = min(U, x.u0 + (hi - p));
+    x.h = seg / blocks;
+    x.row0 = seg % blocks * rb;
+    x.whole = x.u0 == 0u && x.u1 == U;
+    x.part = 2u * t + (p == lo && x.u0 != 0u ? 0u : 1u);
+    return x;
 }
 
-// D: head dimension.  NB: blocks of 16 query rows of a wavefront.  WQ: groups
-// of wavefronts with different rows (the other 4 / WQ share rows and take
-// every (4 / WQ)-th step).
-template <int DT, int D, int NB, int WQ>
-__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend(
-    AttArgs a, uint32_t n_tiles, Gate g)
+// The pages of a step: those of its first and last 16 tokens (a block holds
+// whole groups of 16).  Pages past the cache's end are not looked up: their
+// entries may hold anything.
+struct StepPages {
+    uint32_t e[2];
+};
+
+__device__ __forceinline__ StepPages step_pages(const uint32_t *row_table, const Piece &x, uint32_t u, uint32_t bshift)
 {
-    constexpr uint32_t WK = kAttWaves / WQ;
-    constexpr uint32_t kRows = 16u * NB * WQ;  // rows of a segment
-    constexpr int KK = D / 32;                 // MFMA steps along the head
-    constexpr int DD = D / 16;                 // blocks of 16 dims of O^T
-    // f16's P is scaled by 2^10: weights down to 2^-34 of the largest stay
-    // normal or subnormal numbers there (bf16 has fp32's range)
-    constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
+    const uint32_t last = x.total ? (x.total - 1u) >> bshift : 0u;
+    StepPages s;
+#pragma unroll
+    for (uint32_t i = 0; i < 2u; ++i)
+        s.e[i] = __builtin_amdgcn_readfirstlane(row_table[min((u * kStep + 16u * i) >> bshift, last)]);
+    return s;
+}
+
+// The head's chunks on a step's pages.  ``bad``: bit i set where the pool
+// does not have page i (then page 0, whose values are not used), both set
+// for a cache without tokens.
+struct StepAt {
+    const uint8_t *p[2];
+    uint32_t bad;
+};
+
+__device__ __forceinline__ StepAt step_at(const AttArgs &a, const uint8_t *head, const StepPages &s, uint32_t total,
+                                          uint32_t &err)
+{
+    StepAt at;
+    at.bad = 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < 2u; ++i) {
+        const bool bad = (uint64_t)s.e[i] >= a.c.pool_pages;
+        at.bad |= bad || total == 0u ? 1u << i : 0u;
+        err |= bad && total != 0u ? kDevErrPtRange : 0u;
+        at.p[i] = head + ((uint64_t)(bad || total == 0u ? 0u : s.e[i]) << a.c.shift);
+    }
+    return at;
+}
+
+// A wavefront's rows: column ``col`` of block b is row row0 + 16 b + col of
+// the request, node row / group, query head h group + row % group.
+template <int DT, int D, int NB>
+struct Rows {
+    u32x4 q[NB][D / 32];
+    f32x4 acc[NB][D / 16];      // O^T: dims 16 dd + 4 grp .. + 3 of column col
+    float m[NB], l[NB];
+    uint32_t tok[NB], node[NB];
+
+    __device__ __forceinline__ void begin(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t col, uint32_t grp)
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const uint32_t row = min(row0 + 16u * b + col, x.rows - 1u);
+            node[b] = row / a.group;
+            tok[b] = x.start + node[b];
+            const uint8_t *const qp = a.q.ptr + tok[b] * a.q.token + (x.h * a.group + row % a.group) * a.q.head;
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+                q[b][kk] = *reinterpret_cast<const u32x4 *>(qp + (kk * 4u + grp) * 16u);
+            m[b] = -INFINITY;
+            l[b] = 0.0f;
+#pragma unroll
+            for (int dd = 0; dd < D / 16; ++dd)
+                acc[b][dd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+};
+
+// Scores capped to cap tanh(s scale / cap), in units of log 2; tanh y = 1 -
+// 2 / (1 + e^2y).
+template <int NB>
+__device__ __forceinline__ void cap_scores(const AttArgs &a, f32x4 (&s)[NB][2])
+{
+    const float in = a.scale / a.softcap * 2.0f * kLog2e, out = a.softcap * kLog2e;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(s[b][x][i] * in);
+                s[b][x][i] = out - 2.0f * out * __builtin_amdgcn_rcpf(1.0f + e);
+            }
+}
+
+// f16's P is scaled by 2^10: weights down to 2^-34 of the largest stay normal
+// or subnormal numbers there (bf16 has fp32's range).
+template <int DT>
+constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
+
+// Scores to weights: the running maximum, what was summed under the old one
+// rescaled, the weights added up and rounded to the P^T operand.  A row's
+// sum stays spread over its four lanes until the end.
+template <int DT, int D, int NB>
+__device__ __forceinline__ void weigh(Rows<DT, D, NB> &w, const f32x4 (&s)[NB][2], float c2, u32x4 (&pf)[NB])
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float mx = fmaxf(s[b][0][0], s[b][0][1]);
+#pragma unroll
+        for (int i = 2; i < 8; ++i)
+            mx = fmaxf(mx, s[b][i >> 2][i & 3]);
+        mx = row_max(mx);
+        if (__ballot(mx > w.m[b]) != 0ull) {
+            const float mn = fmaxf(w.m[b], mx);
+            const float f = __builtin_amdgcn_exp2f((w.m[b] - (mn == -INFINITY ? 0.0f : mn)) * c2);
+            w.m[b] = mn;
+            w.l[b] *= f;
+#pragma unroll
+            for (int dd = 0; dd < D / 16; ++dd)
+                w.acc[b][dd] *= f;
+        }
+        const float sub = (w.m[b] == -INFINITY ? 0.0f : w.m[b] * c2) - kLift<DT>;
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i >> 2][i & 3], c2, -sub));
+            w.l[b] += p[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pf[b][i] = pack2<DT>(p[2 * i], p[2 * i + 1]);
+    }
+}
+
+// A step that reaches into the drafted tokens or past the cache's end: which
+// of the lane's eight tokens its rows see (``there``: those that exist).
+template <int DT, int D, int NB>
+__device__ __forceinline__ void mask_scores(const AttArgs &a, const Rows<DT, D, NB> &w, int32_t j0, int32_t drafted,
+                                            uint32_t there, f32x4 (&s)[NB][2], uint32_t (&seen)[NB])
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        seen[b] = seen8(a, w.tok[b], w.node[b], j0, drafted) & there;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            s[b][i >> 2][i & 3] = (seen[b] >> i) & 1u ? s[b][i >> 2][i & 3] : -INFINITY;
+    }
+}
+
+// O^T += V^T P^T where infinities or NaN among the drafted values must not
+// meet the weight 0 of a row that does not see them.  They are taken out of V,
+// and a product of marks counts those that each row sees: such a sum is
+// infinite or NaN, whatever the rest is.  ``load_v(dd)``: V^T's operand.
+template <int DT, int D, int NB, typename LoadV>
+__device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[NB], const uint32_t (&seen)[NB],
+                                        LoadV load_v)
+{
+    u32x4 some[NB], none[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t sees = pair_mask(seen[b], w), weight = spread_top(top_from<1u>(pf[b][w]));
+            some[b][w] = sees & weight & kOne<DT>;
+            none[b][w] = sees & ~weight & kOne<DT>;
+        }
+#pragma unroll
+    for (int dd = 0; dd < D / 16; ++dd) {
+        u32x4 v = load_v(dd), marks;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t two = v[w];
+            marks[w] = take_marks<DT>(two);
+            v[w] = two;
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+            r.acc[b][dd] = att_mfma<DT>(v, pf[b], r.acc[b][dd]);
+            const f32x4 n = att_mfma<DT>(marks, some[b], z), n0 = att_mfma<DT>(marks, none[b], z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r.acc[b][dd][i] += marked(n[i], n0[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // one block's marks at a time
+    }
+}
+
+// Zeroes what does not exist (``there``: bits of 8 tokens) in 16 bytes of V;
+// not zero if a value that is left is infinite or NaN.
+template <int DT>
+__device__ __forceinline__ uint32_t keep_there(u32x4 &v, uint32_t there)
+{
+    uint32_t odd = 0u;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        v[w] &= pair_mask(there, w);
+        odd |= top_from<kInf<DT>>(v[w]);
+    }
+    return odd;
+}
+
+// The end of a piece: joins the WK wavefronts that shared rows (maxima and
+// sums first, then the weighted V, 16 rows at a time) and writes the rows, or
+// the partial result.  NW wavefronts; wavefront ``wave`` has rows 16 NB (wave
+// / WK) .. of the segment.  Ends with a barrier.
+template <int DT, int D, int NB, uint32_t NW, uint32_t WK>
+__device__ __forceinline__ void end_piece(const AttArgs &a, const Piece &x, Rows<DT, D, NB> &w, float c2,
+                                          float (*s_ml)[16 * NB][2], float (*s_o)[16][D + 4], uint32_t wave)
+{
+    constexpr uint32_t kRows = 16u * NB * NW / WK;
+    const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, grp = lane >> 4;
+    const uint32_t wq = wave / WK;
+    float f[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        w.l[b] = row_sum(w.l[b]);
+        if (grp == 0u) {
+            s_ml[wave][16 * b + col][0] = w.m[b];
+            s_ml[wave][16 * b + col][1] = w.l[b];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float mj = -INFINITY;
+#pragma unroll
+        for (uint32_t k = 0; k < WK; ++k)
+            mj = fmaxf(mj, s_ml[wq * WK + k][16 * b + col][0]);
+        const float use = mj == -INFINITY ? 0.0f : mj;
+        float lj = 0.0f;
+#pragma unroll
+        for (uint32_t k = 0; k < WK; ++k)
+            lj += s_ml[wq * WK + k][16 * b + col][1] *
+                  __builtin_amdgcn_exp2f((s_ml[wq * WK + k][16 * b + col][0] - use) * c2);
+        f[b] = __builtin_amdgcn_exp2f((w.m[b] - use) * c2);
+        if (x.whole)
+            f[b] = lj > 0.0f ? f[b] / lj : lj == 0.0f ? 0.0f : lj;  // NaN stays NaN
+        const uint32_t in = 16u * (wq * NB + b) + col;
+        if (wave % WK == 0u && grp == 0u && x.row0 + in < x.rows) {
+            if (!x.whole) {
+                float *const st = part_stats(a.work, x.part, kRows, D) + in * 2u;
+                st[0] = mj;
+                st[1] = lj;
+            } else if (a.lse) {
+                a.lse[(uint64_t)w.tok[b] * a.heads + x.h * a.group + (x.row0 + in) % a.group] =
+                    lj == 0.0f ? -INFINITY : (mj * c2 - kLift<DT> + __log2f(lj)) * kLn2;
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int dd = 0; dd < D / 16; ++dd)
+            *reinterpret_cast<f32x4 *>(&s_o[wave][col][dd * 16 + grp * 4u]) = w.acc[b][dd] * f[b];
+        __syncthreads();
+        // each group of WK wavefronts adds up its own 16 rows, 4 dims a thread
+        for (uint32_t i = threadIdx.x % (64u * WK); i < 16u * (D / 4); i += 64u * WK) {
+            const uint32_t rr = i / (D / 4), d = i % (D / 4) * 4u;
+            const uint32_t in = 16u * (wq * NB + b) + rr, row = x.row0 + in;
+            f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[wq * WK][rr][d]);
+#pragma unroll
+            for (uint32_t k = 1; k < WK; ++k)
+                v += *reinterpret_cast<const f32x4 *>(&s_o[wq * WK + k][rr][d]);
+            if (row < x.rows) {
+                if (x.whole) {
+                    uint8_t *const op = a.o + (x.start + row / a.group) * a.o_token +
+                                        (x.h * a.group + row % a.group) * a.o_head + d * 2u;
+                    const u32x2 two = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+                    *reinterpret_cast<u32x2 *>(op) = two;
+                } else {
+                    *reinterpret_cast<f32x4 *>(part_rows(a.work, x.part, kRows, D) + (uint64_t)in * D + d) = v;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Few rows (16 NB of a segment at most): bound by the cache's bytes.  The four
+// wavefronts share the rows and take every fourth step.  K and V go from
+// memory to the MFMA operands' registers; the next step's K is requested as
+// soon as the scores have taken this one's, the next V after the products with
+// this one, into the same registers, so that a wavefront has a step in flight
+// for the registers of one.
+template <int DT, int D, int NB>
+__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend_few(AttArgs a, uint32_t n_tiles, Gate g)
+{
+    constexpr uint32_t WK = kAttWaves;
+    constexpr int KK = D / 32, DD = D / 16;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
     __shared__ float s_ml[kAttWaves][16 * NB][2];
@@ -298,287 +612,248 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t col = lane & 15u, grp = lane >> 4;
-    const uint32_t wq = wave / WK, wk = wave % WK;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
     uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line(a, kRows, s_line, s_sum, pro_err); };
+    auto prologue = [&]() { plan_line<kAttThreads>(a, 16u * NB, s_line, s_sum, pro_err); };
     auto body = [&](uint32_t t, uint32_t &err) {
         err |= pro_err;
         const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
-        const uint32_t ranges = n_ranges(steps);
+        const uint32_t ranges = n_ranges(a, steps);
         const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
         const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
         for (uint32_t p = lo; p < hi;) {
-            const uint32_t r = __builtin_amdgcn_readfirstlane(find_request(s_line, a.n_requests, p));
-            const Req rq = load_req(a, r);
-            const uint32_t U = __builtin_amdgcn_readfirstlane(seg_steps(rq));
-            const uint32_t total = __builtin_amdgcn_readfirstlane(rq.total);
-            const uint32_t ctx = __builtin_amdgcn_readfirstlane(rq.ctx);
-            const uint32_t rows = __builtin_amdgcn_readfirstlane(rq.nodes * a.group);
-            const uint32_t start = __builtin_amdgcn_readfirstlane(rq.start);
-            const uint32_t blocks = (rows + kRows - 1u) / kRows;
-            const uint32_t at = p - __builtin_amdgcn_readfirstlane(s_line[r]);
-            const uint32_t seg = at / U, u0 = at % U;
-            const uint32_t h = seg / blocks, row0 = seg % blocks * kRows;
-            const uint32_t u1 = min(U, u0 + (hi - p));
-            const bool first = p == lo;
-            p += u1 - u0;
-
-            // this wavefront's rows of Q: column ``col`` of block b is row
-            // row0 + 16 (wq NB + b) + col, node row / group
-            u32x4 qf[NB][KK];
-            uint32_t tok[NB], node[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const uint32_t row = min(row0 + 16u * (wq * NB + b) + col, rows - 1u);
-                node[b] = row / a.group;
-                tok[b] = start + node[b];
-                const uint8_t *const qp = a.q.ptr + tok[b] * a.q.token + (h * a.group + row % a.group) * a.q.head;
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    qf[b][kk] = *reinterpret_cast<const u32x4 *>(qp + (kk * 4u + grp) * 16u);
-            }
-            f32x4 acc[NB][DD];
-            float m[NB], l[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                m[b] = -INFINITY;
-                l[b] = 0.0f;
-#pragma unroll
-                for (int dd = 0; dd < DD; ++dd)
-                    acc[b][dd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-            const uint32_t *const row_table = a.table + (uint64_t)r * a.stride;
-            const uint32_t last_block = total ? (total - 1u) >> a.c.bshift : 0u;
-            // K's lanes: token 8 (col / 4) + col % 4 (+ 4) of the step
-            const uint32_t k_tok = (col >> 2) * 8u + (col & 3u);
-            const uint8_t *const head = a.c.pool + h * head_bytes<D>(a.c.bshift);
+            const Piece x = take_piece(a, s_line, 16u * NB, t, lo, hi, p);
+            p += x.u1 - x.u0;
+            Rows<DT, D, NB> w;
+            w.begin(a, x, 0u, col, grp);
+            const uint32_t *const row_table = a.table + (uint64_t)x.r * a.stride;
+            const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
             const uint32_t bmask = (1u << a.c.bshift) - 1u;
-
-            for (uint32_t u = u0 + wk; u < u1; u += WK) {
-                const uint32_t base = u * kStep;
-                // a block holds whole groups of 8 tokens; pages past the cache's
-                // end are not looked up (their entries may hold anything)
-                uint32_t bad = 0u, bad_k = 0u;
-                const uint32_t ke = checked_page(row_table, min((base + (col >> 2) * 8u) >> a.c.bshift, last_block),
-                                                 a.c.pool_pages, bad_k);
-                const uint32_t ve = checked_page(row_table, min((base + grp * 8u) >> a.c.bshift, last_block),
-                                                 a.c.pool_pages, bad);
-                if (total == 0u)
-                    bad = bad_k = 1u;
-                else
-                    err |= bad;
-                const uint8_t *const kp = head + ((uint64_t)(bad_k ? 0u : ke) << a.c.shift);
-                const uint8_t *const vp = head + ((uint64_t)(bad ? 0u : ve) << a.c.shift);
-                const uint32_t kt = (base + k_tok) & bmask, vt = ((base + grp * 8u) & bmask) >> 3;
-                u32x4 kf[2][KK], vf[DD];
+            const int32_t drafted = (int32_t)(x.total - x.ctx);
+            // K's lanes: token 8 (col / 4) + col % 4 (+ 4) of a step, in its
+            // half col / 8; V's: tokens 8 grp .. + 7, in half grp / 2
+            const uint32_t k_tok = (col >> 2) * 8u + (col & 3u);
+            const uint32_t k_lane = k_off<D>(grp, k_tok & bmask, a.c.bshift);
+            const uint32_t v_lane = v_off<D>((grp * 8u & bmask) >> 3, col, a.c.bshift);
+            u32x4 kf[2][KK], vf[DD];
+            auto load_k = [&](uint32_t u, const StepAt &at) __attribute__((always_inline)) {
+                const uint8_t *const kp = (col < 8u ? at.p[0] : at.p[1]) + k_lane + (u * kStep & bmask) * 16u;
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) {
-                    kf[0][kk] = *reinterpret_cast<const u32x4 *>(kp + k_off<D>(kk * 4u + grp, kt, a.c.bshift));
-                    kf[1][kk] = *reinterpret_cast<const u32x4 *>(kp + k_off<D>(kk * 4u + grp, kt + 4u, a.c.bshift));
+                    kf[0][kk] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)kk * 64u << a.c.bshift));
+                    kf[1][kk] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)kk * 64u << a.c.bshift) + 64u);
                 }
+            };
+            auto load_v = [&](uint32_t u, const StepAt &at) __attribute__((always_inline)) {
+                const uint8_t *const vp = (grp < 2u ? at.p[0] : at.p[1]) + v_lane + (u * kStep & bmask) * (2u * D);
 #pragma unroll
                 for (int dd = 0; dd < DD; ++dd)
-                    vf[dd] = *reinterpret_cast<const u32x4 *>(vp + v_off<D>(vt, dd * 16u + col, a.c.bshift));
-
-                f32x4 s[NB][2];
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        s[b][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int kk = 0; kk < KK; ++kk)
-                            s[b][x] = att_mfma<DT>(kf[x][kk], qf[b][kk], s[b][x]);
-                    }
-                if (a.softcap > 0.0f) {
-                    // cap tanh(s scale / cap) in units of log 2; tanh y = 1 - 2 / (1 + e^2y)
-                    const float in = a.scale / a.softcap * 2.0f * kLog2e, out = a.softcap * kLog2e;
+                    vf[dd] = *reinterpret_cast<const u32x4 *>(vp + dd * 256);
+            };
+            uint32_t u = x.u0 + wave;
+            if (u < x.u1) {
+                StepAt at = step_at(a, head, step_pages(row_table, x, u, a.c.bshift), x.total, err);
+                load_k(u, at);
+                load_v(u, at);
+                StepPages ahead = step_pages(row_table, x, min(u + WK, x.u1 - 1u), a.c.bshift);
+                for (; u < x.u1; u += WK) {
+                    f32x4 s[NB][2];
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
-                        for (int x = 0; x < 2; ++x)
+                        for (int q = 0; q < 2; ++q) {
+                            s[b][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float e = __builtin_amdgcn_exp2f(s[b][x][i] * in);
-                                s[b][x][i] = out - 2.0f * out * __builtin_amdgcn_rcpf(1.0f + e);
-                            }
-                }
-                const int32_t j0 = (int32_t)(base + grp * 8u) - (int32_t)ctx;
-                const int32_t drafted = (int32_t)total - (int32_t)ctx;
-                const bool edge = base + kStep > ctx || __ballot(bad != 0u) != 0ull;
-                uint32_t seen[NB];
-                bool odd = false;  // a value that must not meet a weight of zero
-                if (edge) {
-                    const uint32_t there = bad ? 0u : low8(drafted - j0);
-#pragma unroll
-                    for (int dd = 0; dd < DD; ++dd)
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const uint32_t two = (there >> (2 * w)) & 3u;
-                            vf[dd][w] &= (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
-                            odd = odd || not_finite2<DT>(vf[dd][w]);
+                            for (int kk = 0; kk < KK; ++kk)
+                                s[b][q] = att_mfma<DT>(kf[q][kk], w.q[b][kk], s[b][q]);
                         }
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        seen[b] = seen8(a, tok[b], node[b], j0, drafted) & there;
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                s[b][x][i] = (seen[b] >> (4 * x + i)) & 1u ? s[b][x][i] : -INFINITY;
-                    }
-                }
-                u32x4 pf[NB];
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    float mx = s[b][0][0];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            mx = fmaxf(mx, s[b][x][i]);
-                    mx = row_max(mx);
-                    if (__ballot(mx > m[b]) != 0ull) {
-                        const float mn = fmaxf(m[b], mx);
-                        const float use = mn == -INFINITY ? 0.0f : mn;
-                        const float f = __builtin_amdgcn_exp2f((m[b] - use) * c2);
-                        m[b] = mn;
-                        l[b] *= f;
+                    // the next step; past the piece's end its last one again
+                    const uint32_t bad = at.bad, un = min(u + WK, x.u1 - 1u);
+                    at = step_at(a, head, ahead, x.total, err);
+                    load_k(un, at);
+                    ahead = step_pages(row_table, x, min(u + 2u * WK, x.u1 - 1u), a.c.bshift);
+                    if (a.softcap > 0.0f)
+                        cap_scores<NB>(a, s);
+                    u32x4 pf[NB];
+                    if (u * kStep + kStep <= x.ctx && bad == 0u) {
+                        weigh<DT, D, NB>(w, s, c2, pf);
 #pragma unroll
                         for (int dd = 0; dd < DD; ++dd)
-                            acc[b][dd] *= f;
-                    }
-                    const float sub = (m[b] == -INFINITY ? 0.0f : m[b] * c2) - kLift;
-                    float pv[8];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
+                            for (int b = 0; b < NB; ++b)
+                                w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
+                    } else {
+                        const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
+                        const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
+                        uint32_t odd = 0u;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float e = __builtin_amdgcn_exp2f(s[b][x][i] * c2 - sub);
-                            pv[4 * x + i] = e;
-                            l[b] += e;
+                        for (int dd = 0; dd < DD; ++dd)
+                            odd |= keep_there<DT>(vf[dd], there);
+                        uint32_t seen[NB];
+                        mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
+                        weigh<DT, D, NB>(w, s, c2, pf);
+                        if (__ballot(odd != 0u) != 0ull) {
+                            add_odd<DT, D, NB>(w, pf, seen, [&](int dd) { return vf[dd]; });
+                        } else {
+#pragma unroll
+                            for (int dd = 0; dd < DD; ++dd)
+#pragma unroll
+                                for (int b = 0; b < NB; ++b)
+                                    w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
                         }
-#pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        pf[b][w] = pack2<DT>(pv[2 * w], pv[2 * w + 1]);
+                    }
+                    load_v(un, at);
                 }
-                if (edge && __ballot(odd) != 0ull) {
-                    // infinities or NaN among the drafted values must not meet the
-                    // weight 0 of a row that does not see them.  They are taken
-                    // out of V, and a product of marks counts those that each row
-                    // sees: such a sum is infinite or NaN, whatever the rest is
-                    u32x4 some[NB], none[NB];
+            }
+            end_piece<DT, D, NB, kAttWaves, WK>(a, x, w, c2, s_ml, s_o, wave);
+        }
+    };
+    single_tile_loop(g, n_tiles, prologue, body);
+}
+
+// Many rows: NW wavefronts of 16 NB rows each take the same steps, whose K and
+// V pass through LDS once for all of them.  Every thread moves its share of a
+// step, 16 bytes at a time, in the order of memory, which is the order of the
+// MFMA operands: two steps ahead into registers, then to one of two LDS
+// buffers, so that one barrier a step is enough.
+template <int DT, int D, int NB, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttArgs a, uint32_t n_tiles, Gate g)
+{
+    constexpr uint32_t T = 64u * NW;
+    constexpr uint32_t kRows = 16u * NB * NW;
+    constexpr int KK = D / 32, DD = D / 16;
+    constexpr uint32_t kPieces = 8u * D;                     // of 16 bytes: K's, then V's
+    constexpr uint32_t PER = (kPieces + T - 1u) / T;         // a thread's
+    constexpr uint32_t kBuf = kPieces * 16u;
+    constexpr uint32_t kOut = NW * 16u * (D + 4u) * 4u;
+    __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
+    __shared__ uint32_t s_sum[NW];
+    __shared__ float s_ml[NW][16 * NB][2];
+    // two steps, and at a piece's end the rows' results
+    __shared__ __attribute__((aligned(16))) uint8_t s_kv[2u * kBuf > kOut ? 2u * kBuf : kOut];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t col = lane & 15u, grp = lane >> 4;
+    const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
+    uint32_t pro_err = 0u;
+    auto prologue = [&]() { plan_line<T>(a, kRows, s_line, s_sum, pro_err); };
+    const uint32_t bmask = (1u << a.c.bshift) - 1u;
+    // piece j of this thread: which half of the step it lies in, its place in
+    // the head's chunk, and what a token further is
+    auto half_of = [&](uint32_t i) { return (i < kPieces / 2u ? i % 32u >> 4 : (i - kPieces / 2u) / D >> 1); };
+    auto place_of = [&](uint32_t i) {
+        return i < kPieces / 2u ? k_off<D>(i / 32u, i % 32u & bmask, a.c.bshift)
+                                : v_off<D>(((i - kPieces / 2u) / D * 8u & bmask) >> 3, i % D, a.c.bshift);
+    };
+    static_assert((kPieces / 2u) % D == 0u && kPieces / 2u % 32u == 0u, "V's pieces begin a row");
+    auto body = [&](uint32_t t, uint32_t &err) {
+        err |= pro_err;
+        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
+        const uint32_t ranges = n_ranges(a, steps);
+        const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
+        const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
+        for (uint32_t p = lo; p < hi;) {
+            const Piece x = take_piece(a, s_line, kRows, t, lo, hi, p);
+            p += x.u1 - x.u0;
+            Rows<DT, D, NB> w;
+            w.begin(a, x, x.row0 + 16u * NB * wave, col, grp);
+            const uint32_t *const row_table = a.table + (uint64_t)x.r * a.stride;
+            const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
+            const int32_t drafted = (int32_t)(x.total - x.ctx);
+            u32x4 st[2][PER];
+            uint32_t bads[2] = {0u, 0u};
+            auto fetch = [&](uint32_t u, const StepPages &sp, u32x4 (&to)[PER], uint32_t &bad) __attribute__((always_inline)) {
+                const StepAt at = step_at(a, head, sp, x.total, err);
+                bad = at.bad;
+                const uint32_t off = u * kStep & bmask;
+#pragma unroll
+                for (uint32_t j = 0; j < PER; ++j) {
+                    const uint32_t i = j * T + threadIdx.x;
+                    if (kPieces % T == 0u || i < kPieces)
+                        to[j] = *reinterpret_cast<const u32x4 *>(
+                            (half_of(i) ? at.p[1] : at.p[0]) + place_of(i) + off * (i < kPieces / 2u ? 16u : 2u * D));
+                }
+            };
+            auto step = [&](uint32_t u, u32x4 (&from)[PER], uint32_t &bad_of, uint8_t *buf, StepPages &ahead) __attribute__((always_inline)) {
+                const uint32_t bad = bad_of;
+                const bool edge = u * kStep + kStep > x.ctx || bad != 0u;
+                uint32_t odd = 0u;
+                if (edge) {
+#pragma unroll
+                    for (uint32_t j = 0; j < PER; ++j) {
+                        const uint32_t i = j * T + threadIdx.x;
+                        if (i >= kPieces / 2u && i < kPieces) {
+                            const uint32_t t8 = (i - kPieces / 2u) / D;
+                            const int32_t j0 = (int32_t)(u * kStep + t8 * 8u) - (int32_t)x.ctx;
+                            odd |= keep_there<DT>(from[j], (bad >> (t8 >> 1)) & 1u ? 0u : low8(drafted - j0));
+                        }
+                    }
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < PER; ++j) {
+                    const uint32_t i = j * T + threadIdx.x;
+                    if (kPieces % T == 0u || i < kPieces)
+                        *reinterpret_cast<u32x4 *>(buf + i * 16u) = from[j];
+                }
+                if (edge)
+                    odd = (uint32_t)__syncthreads_or((int)(odd != 0u));
+                else
+                    __syncthreads();
+                if (u + 2u < x.u1) {
+                    fetch(u + 2u, ahead, from, bad_of);
+                    ahead = step_pages(row_table, x, min(u + 3u, x.u1 - 1u), a.c.bshift);
+                }
+                const uint8_t *const kb = buf + (grp * 32u + (col >> 2) * 8u + (col & 3u)) * 16u;
+                const uint8_t *const vb = buf + kBuf / 2u + (grp * D + col) * 16u;
+                f32x4 s[NB][2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
+                        s[b][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (uint32_t w = 0; w < 4u; ++w) {
-                            some[b][w] = none[b][w] = 0u;
-#pragma unroll
-                            for (uint32_t i = 0; i < 2u; ++i)
-                                if ((seen[b] >> (2u * w + i)) & 1u) {
-                                    const bool zero = ((pf[b][w] >> (16u * i)) & 0xFFFFu) == 0u;
-                                    some[b][w] |= zero ? 0u : kOne<DT> << (16u * i);
-                                    none[b][w] |= zero ? kOne<DT> << (16u * i) : 0u;
-                                }
-                        }
-#pragma unroll
-                    for (int dd = 0; dd < DD; ++dd) {
-                        u32x4 marks;
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            uint32_t two = vf[dd][w];
-                            marks[w] = take_marks<DT>(two);
-                            vf[dd][w] = two;
-                        }
-#pragma unroll
-                        for (int b = 0; b < NB; ++b) {
-                            const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-                            acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], acc[b][dd]);
-                            const f32x4 n = att_mfma<DT>(marks, some[b], z), n0 = att_mfma<DT>(marks, none[b], z);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                acc[b][dd][i] += marked(n[i], n0[i]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);  // one block's marks at a time
-                    }
-                } else {
-#pragma unroll
-                    for (int dd = 0; dd < DD; ++dd)
+                    for (int kk = 0; kk < KK; ++kk) {
+                        const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + q * 64);
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], acc[b][dd]);
-                }
-            }
-
-            // Join the wavefronts that shared the rows: maxima and sums first,
-            // then the weighted V, 16 rows at a time.
-            float f[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                l[b] = row_sum(l[b]);
-                if (grp == 0u) {
-                    s_ml[wave][16 * b + col][0] = m[b];
-                    s_ml[wave][16 * b + col][1] = l[b];
-                }
-            }
-            __syncthreads();
-            const bool whole = u0 == 0u && u1 == U;
-            const uint32_t part = 2u * t + (first && u0 != 0u ? 0u : 1u);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                float mj = -INFINITY;
-#pragma unroll
-                for (uint32_t w = 0; w < WK; ++w)
-                    mj = fmaxf(mj, s_ml[wq * WK + w][16 * b + col][0]);
-                const float use = mj == -INFINITY ? 0.0f : mj;
-                float lj = 0.0f;
-#pragma unroll
-                for (uint32_t w = 0; w < WK; ++w)
-                    lj += s_ml[wq * WK + w][16 * b + col][1] *
-                          __builtin_amdgcn_exp2f((s_ml[wq * WK + w][16 * b + col][0] - use) * c2);
-                f[b] = __builtin_amdgcn_exp2f((m[b] - use) * c2);
-                if (whole)
-                    f[b] = lj > 0.0f ? f[b] / lj : lj == 0.0f ? 0.0f : lj;  // NaN stays NaN
-                const uint32_t in = 16u * (wq * NB + b) + col;
-                if (wk == 0u && grp == 0u && row0 + in < rows) {
-                    if (!whole) {
-                        float *const st = part_stats(a.work, part, kRows, D) + in * 2u;
-                        st[0] = mj;
-                        st[1] = lj;
-                    } else if (a.lse) {
-                        a.lse[(uint64_t)tok[b] * a.heads + h * a.group + (row0 + in) % a.group] =
-                            lj == 0.0f ? -INFINITY : (mj * c2 - kLift + __log2f(lj)) * kLn2;
+                            s[b][q] = att_mfma<DT>(kf, w.q[b][kk], s[b][q]);
                     }
                 }
-            }
+                if (a.softcap > 0.0f)
+                    cap_scores<NB>(a, s);
+                u32x4 pf[NB];
+                uint32_t seen[NB];
+                if (edge) {
+                    const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
+                    const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
+                    mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
+                }
+                weigh<DT, D, NB>(w, s, c2, pf);
+                if (odd != 0u) {
+                    add_odd<DT, D, NB>(w, pf, seen, [&](int dd) {
+                        return *reinterpret_cast<const u32x4 *>(vb + dd * 256);
+                    });
+                } else {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
+                    for (int dd = 0; dd < DD; ++dd) {
+                        const u32x4 vf = *reinterpret_cast<const u32x4 *>(vb + dd * 256);
 #pragma unroll
-                for (int dd = 0; dd < DD; ++dd)
-                    *reinterpret_cast<f32x4 *>(&s_o[wave][col][dd * 16 + grp * 4u]) = acc[b][dd] * f[b];
-                __syncthreads();
-                // each group of WK wavefronts adds up its own 16 rows, 4 dims a thread
-                for (uint32_t i = threadIdx.x % (64u * WK); i < 16u * (D / 4); i += 64u * WK) {
-                    const uint32_t x = i / (D / 4), d = i % (D / 4) * 4u;
-                    const uint32_t in = 16u * (wq * NB + b) + x, row = row0 + in;
-                    f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[wq * WK][x][d]);
-#pragma unroll
-                    for (uint32_t w = 1; w < WK; ++w)
-                        v += *reinterpret_cast<const f32x4 *>(&s_o[wq * WK + w][x][d]);
-                    if (row < rows) {
-                        if (whole) {
-                            uint8_t *const op = a.o + (start + row / a.group) * a.o_token +
-                                                (h * a.group + row % a.group) * a.o_head + d * 2u;
-                            const u32x2 two = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
-                            *reinterpret_cast<u32x2 *>(op) = two;
-                        } else {
-                            *reinterpret_cast<f32x4 *>(part_rows(a.work, part, kRows, D) + (uint64_t)in * D + d) = v;
-                        }
+                        for (int b = 0; b < NB; ++b)
+                            w.acc[b][dd] = att_mfma<DT>(vf, pf[b], w.acc[b][dd]);
                     }
                 }
-                __syncthreads();
+            };
+            fetch(x.u0, step_pages(row_table, x, x.u0, a.c.bshift), st[0], bads[0]);
+            fetch(min(x.u0 + 1u, x.u1 - 1u), step_pages(row_table, x, min(x.u0 + 1u, x.u1 - 1u), a.c.bshift), st[1],
+                  bads[1]);
+            StepPages ahead = step_pages(row_table, x, min(x.u0 + 2u, x.u1 - 1u), a.c.bshift);
+            for (uint32_t u = x.u0; u < x.u1; u += 2u) {
+                step(u, st[0], bads[0], s_kv, ahead);
+                if (u + 1u < x.u1)
+                    step(u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
             }
+            __syncthreads();  // the last step is read: its LDS becomes the results'
+            end_piece<DT, D, NB, NW, 1>(a, x, w, c2, s_ml, reinterpret_cast<float(*)[16][D + 4]>(s_kv), wave);
         }
     };
     single_tile_loop(g, n_tiles, prologue, body);
@@ -591,7 +866,6 @@ constexpr uint32_t kJoinRows = 4;  // rows of a join tile, one a wavefront
 template <int DT, int D>
 __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t rb, uint32_t n_tiles, Gate g)
 {
-    constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
     constexpr uint32_t PER = (D + 63) / 64;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
@@ -599,7 +873,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
     const uint32_t lane = threadIdx.x & 63u;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
     uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line(a, rb, s_line, s_sum, pro_err); };
+    auto prologue = [&]() { plan_line<kAttThreads>(a, rb, s_line, s_sum, pro_err); };
     auto body = [&](uint32_t t, uint32_t &) {
         const uint64_t i = (uint64_t)t * kJoinRows + wave;
         const uint32_t token = (uint32_t)(i / a.heads), qh = (uint32_t)(i % a.heads);
@@ -617,7 +891,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
         const Req rq = load_req(a, r);
         const bool mine = token < a.n_tokens && token >= rq.start && token - rq.start < rq.nodes && steps != 0u;
         const uint32_t node = token - rq.start;
-        const uint32_t ranges = n_ranges(steps);
+        const uint32_t ranges = n_ranges(a, steps);
         uint32_t t0 = 0u, t1 = 0u, in = 0u, seg0 = 0u;
         if (mine) {
             const uint32_t row = node * a.group + qh % a.group;
@@ -670,7 +944,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
                     *reinterpret_cast<uint16_t *>(op + (lane + 64u * e) * 2u) = (uint16_t)pack2<DT>(v[e] * inv, 0.0f);
             if (a.lse && lane == 0u)
                 a.lse[(uint64_t)token * a.heads + qh] =
-                    l == 0.0f ? -INFINITY : (mx * c2 - kLift + __log2f(l)) * kLn2;
+                    l == 0.0f ? -INFINITY : (mx * c2 - kLift<DT> + __log2f(l)) * kLn2;
         }
     };
     single_tile_loop(g, n_tiles, prologue, body);
@@ -681,38 +955,44 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
 typedef void (*AttKernel)(AttArgs, uint32_t, Gate);
 typedef void (*JoinKernel)(AttArgs, uint32_t, uint32_t, Gate);
 
-// How a call's rows are spread: rows = 16 nb wq of a segment.
+// How a call's rows are spread, by the most rows a segment can have: the
+// kernel, its wavefronts, blocks of 16 rows of each, and the ranges that the
+// line of steps is cut in (as many as workgroups fit on 256 CUs).
 struct AttForm {
-    uint32_t nb, wq;
+    bool many;
+    uint32_t nb, waves, ranges;
+
+    uint32_t rows() const { return 16u * nb * (many ? waves : 1u); }
 };
 
 static AttForm att_form(uint32_t dim, uint32_t rows)
 {
     if (rows <= 16u)
-        return {1, 1};
-    if (rows <= 32u)
-        return {2, 1};
-    if (dim == 256u)  // four blocks of rows would not fit the registers
-        return rows <= 64u ? AttForm{2, 2} : AttForm{2, 4};
+        return {false, 1, 4, dim == 256u ? 256u : 512u};
+    if (rows <= 32u && dim != 256u)
+        return {false, 2, 4, 256};
     if (rows <= 64u)
-        return {4, 1};
-    return rows <= 128u ? AttForm{4, 2} : AttForm{4, 4};
+        return {true, 1, 4, 512};
+    if (dim == 256u || rows <= 128u)
+        return {true, 1, 8, 256};
+    return {true, 2, 8, 256};
 }
 
 template <int DT, int D>
 static AttKernel att_kernel_d(AttForm f)
 {
-    if (f.nb == 1)
-        return k_attend<DT, D, 1, 1>;
-    if (f.nb == 2 && f.wq == 1)
-        return k_attend<DT, D, 2, 1>;
-    if constexpr (D == 256) {
-        return f.wq == 2 ? k_attend<DT, D, 2, 2> : k_attend<DT, D, 2, 4>;
-    } else {
-        if (f.wq == 1)
-            return k_attend<DT, D, 4, 1>;
-        return f.wq == 2 ? k_attend<DT, D, 4, 2> : k_attend<DT, D, 4, 4>;
+    if (!f.many) {
+        if constexpr (D != 256)
+            if (f.nb == 2)
+                return k_attend_few<DT, D, 2>;
+        return k_attend_few<DT, D, 1>;
     }
+    if (f.waves == 4)
+        return k_attend_many<DT, D, 1, 4>;
+    if constexpr (D != 256)
+        if (f.nb == 2)
+            return k_attend_many<DT, D, 2, 8>;
+    return k_attend_many<DT, D, 1, 8>;
 }
 
 template <int DT>
@@ -727,7 +1007,7 @@ static AttKernel att_kernel(uint32_t dim, AttForm f, JoinKernel *join)
 }
 
 template <typename K>
-static int att_occupancy(K k)
+static int att_occupancy(K k, int threads)
 {
     static std::mutex mu;
     static std::unordered_map<const void *, int> cache;
@@ -735,7 +1015,7 @@ static int att_occupancy(K k)
     auto it = cache.find((const void *)k);
     if (it != cache.end())
         return it->second;
-    const int n = occupancy(k, kAttThreads);
+    const int n = occupancy(k, threads);
     cache[(const void *)k] = n;
     return n;
 }
@@ -756,7 +1036,7 @@ static int check_att_shape(const sgdrc_kv_cache *cache, uint32_t n_heads, uint32
 static uint64_t att_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads, uint32_t max_nodes)
 {
     const AttForm f = att_form(cache->head_dim, max_nodes * (n_heads / cache->kv_heads));
-    return 2ull * kRanges * 16u * f.nb * f.wq * (cache->head_dim + 2u) * sizeof(float);
+    return 2ull * f.ranges * f.rows() * (cache->head_dim + 2u) * sizeof(float);
 }
 
 }  // namespace sgdrc
@@ -806,7 +1086,7 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
         return set_error(SGDRC_EINVAL, "n_tokens above 2^31 - 1");
     const uint32_t group = n_heads / cache->kv_heads;
     const AttForm f = att_form(cache->head_dim, max_nodes * group);
-    const uint32_t rb = 16u * f.nb * f.wq;
+    const uint32_t rb = f.rows();
     const uint64_t seg = ((uint64_t)blocks->stride * cache->block_tokens + kStep - 1u) / kStep;
     const uint64_t blocks_of_rows = (max_nodes * group + rb - 1u) / rb;
     if (seg * blocks_of_rows * cache->kv_heads > (1ull << 31) / blocks->n_requests)
@@ -844,21 +1124,24 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     a.group = group;
     a.scale = scale;
     a.softcap = softcap;
+    a.most_ranges = f.ranges;
     JoinKernel join = nullptr;
     const AttKernel k = cache->dtype == SGDRC_BF16 ? att_kernel<SGDRC_BF16>(cache->head_dim, f, &join)
                                                    : att_kernel<SGDRC_F16>(cache->head_dim, f, &join);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     Gate g;
     LaunchInfo li;
-    if ((rc = make_gate(c, stream, kRanges, kStreamGroupCus, &g, &li, false, true)))
+    if ((rc = make_gate(c, stream, f.ranges, kStreamGroupCus, &g, &li, false, true)))
         return rc;
-    hipLaunchKernelGGL(k, dim3(gated_grid(c, att_occupancy(k), kRanges, li)), dim3(kAttThreads), 0, s, a, kRanges, g);
+    const int threads = (int)(64u * f.waves);
+    hipLaunchKernelGGL(k, dim3(gated_grid(c, att_occupancy(k, threads), f.ranges, li)), dim3(threads), 0, s, a, f.ranges,
+                       g);
     SGDRC_HIP(hipGetLastError());
     if ((rc = finish_static_tlog(g, s)))
         return rc;
     if ((rc = make_gate(c, stream, join_tiles, kStreamGroupCus, &g, &li, false, true)))
         return rc;
-    hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join), join_tiles, li)), dim3(kAttThreads), 0, s, a, rb,
+    hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join, kAttThreads), join_tiles, li)), dim3(kAttThreads), 0, s, a, rb,
                        (uint32_t)join_tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);
