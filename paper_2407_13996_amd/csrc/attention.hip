@@ -47,9 +47,6 @@ struct AttArgs {
     uint8_t *o;
     uint64_t o_token, o_head;   // bytes
     float *lse;
-    const uint32_t *q_start;
-    const uint32_t *table;
-    const int32_t *lens, *totals;
     const uint64_t *mask;
     float *work;
     uint32_t n_requests, stride, n_tokens, max_nodes, mask_words;
@@ -58,17 +55,31 @@ struct AttArgs {
     float scale, softcap;
 };
 
+// What the kernels read of the requests.  Kernel arguments of their own,
+// so that the compiler knows that nothing writes them and reads what is the
+// same for a whole wavefront by scalar loads: these have a counter of their
+// own, and waiting for a page-table entry does not wait for the K and V in
+// flight.
+struct Seqs {
+    const uint32_t *q_start, *table;
+    const int32_t *lens, *totals;
+};
+
+#define SGDRC_SEQS_ARGS \
+    const uint32_t *__restrict__ q_start, const uint32_t *__restrict__ table, const int32_t *__restrict__ lens, \
+        const int32_t *__restrict__ totals
+
 // A request as the kernels see it: device values brought into range.
 struct Req {
     uint32_t start, nodes, total, ctx;
     bool ok;
 };
 
-__device__ __forceinline__ Req load_req(const AttArgs &a, uint32_t r)
+__device__ __forceinline__ Req load_req(const AttArgs &a, const Seqs &sq, uint32_t r)
 {
     Req q;
-    const uint32_t s = a.q_start[r], e = a.q_start[r + 1u];
-    const int32_t total = a.totals[r], ctx = a.lens[r];
+    const uint32_t s = sq.q_start[r], e = sq.q_start[r + 1u];
+    const int32_t total = sq.totals[r], ctx = sq.lens[r];
     const uint32_t cap = a.stride << a.c.bshift;
     q.start = min(s, a.n_tokens);
     const uint32_t end = max(min(e, a.n_tokens), q.start);
@@ -95,7 +106,7 @@ __device__ __forceinline__ uint32_t row_blocks(const Req &q, uint32_t group, uin
 // All workgroups: s_line[r] = first step of request r in the line of steps,
 // s_line[n_requests] their number.
 template <uint32_t THREADS>
-__device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_t *s_line, uint32_t *s_sum,
+__device__ __forceinline__ void plan_line(const AttArgs &a, const Seqs &sq, uint32_t rb, uint32_t *s_line, uint32_t *s_sum,
                                           uint32_t &err)
 {
     const uint32_t R = a.n_requests;
@@ -103,7 +114,7 @@ __device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_
     const uint32_t r0 = min(threadIdx.x * per, R), r1 = min(r0 + per, R);
     uint32_t sum = 0u;
     for (uint32_t r = r0; r < r1; ++r) {
-        const Req q = load_req(a, r);
+        const Req q = load_req(a, sq, r);
         err |= q.ok ? 0u : kDevErrSeq;
         sum += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
     }
@@ -121,7 +132,7 @@ __device__ __forceinline__ void plan_line(const AttArgs &a, uint32_t rb, uint32_
     for (uint32_t w = 0; w < wave; ++w)
         run += s_sum[w];
     for (uint32_t r = r0; r < r1; ++r) {
-        const Req q = load_req(a, r);
+        const Req q = load_req(a, sq, r);
         s_line[r] = run;
         run += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
         if (r == R - 1u)
@@ -300,12 +311,12 @@ struct Piece {
 };
 
 // The piece that begins at step ``p`` of the line, in range ``t`` = [lo, hi); all values uniform.
-__device__ __forceinline__ Piece take_piece(const AttArgs &a, const uint32_t *s_line, uint32_t rb, uint32_t t,
+__device__ __forceinline__ Piece take_piece(const AttArgs &a, const Seqs &sq, const uint32_t *s_line, uint32_t rb, uint32_t t,
                                             uint32_t lo, uint32_t hi, uint32_t p)
 {
     Piece x;
     x.r = __builtin_amdgcn_readfirstlane(find_request(s_line, a.n_requests, p));
-    const Req rq = load_req(a, x.r);
+    const Req rq = load_req(a, sq, x.r);
     const uint32_t U = __builtin_amdgcn_readfirstlane(seg_steps(rq));
     x.total = __builtin_amdgcn_readfirstlane(rq.total);
     x.ctx = __builtin_amdgcn_readfirstlane(rq.ctx);
@@ -323,6 +334,14 @@ __device__ __forceinline__ Piece take_piece(const AttArgs &a, const uint32_t *s_
     return x;
 }
 
+// p[i], the same for the whole wavefront and not written by the kernel, by a
+// scalar load.
+__device__ __forceinline__ uint32_t load_uniform(const uint32_t *p, uint32_t i)
+{
+    typedef const uint32_t __attribute__((address_space(4))) *Const;
+    return reinterpret_cast<Const>(reinterpret_cast<uintptr_t>(p))[__builtin_amdgcn_readfirstlane(i)];
+}
+
 // The pages of a step: those of its first and last 16 tokens (a block holds
 // whole groups of 16).  Pages past the cache's end are not looked up: their
 // entries may hold anything.
@@ -336,7 +355,7 @@ __device__ __forceinline__ StepPages step_pages(const uint32_t *row_table, const
     StepPages s;
 #pragma unroll
     for (uint32_t i = 0; i < 2u; ++i)
-        s.e[i] = __builtin_amdgcn_readfirstlane(row_table[min((u * kStep + 16u * i) >> bshift, last)]);
+        s.e[i] = load_uniform(row_table, min((u * kStep + 16u * i) >> bshift, last));
     return s;
 }
 
@@ -601,8 +620,9 @@ __device__ __forceinline__ void end_piece(const AttArgs &a, const Piece &x, Rows
 // this one, into the same registers, so that a wavefront has a step in flight
 // for the registers of one.
 template <int DT, int D, int NB>
-__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend_few(AttArgs a, uint32_t n_tiles, Gate g)
+__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend_few(AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
 {
+    const Seqs sq = {q_start, table, lens, totals};
     constexpr uint32_t WK = kAttWaves;
     constexpr int KK = D / 32, DD = D / 16;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
@@ -614,7 +634,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
     const uint32_t col = lane & 15u, grp = lane >> 4;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
     uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line<kAttThreads>(a, 16u * NB, s_line, s_sum, pro_err); };
+    auto prologue = [&]() { plan_line<kAttThreads>(a, sq, 16u * NB, s_line, s_sum, pro_err); };
     auto body = [&](uint32_t t, uint32_t &err) {
         err |= pro_err;
         const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
@@ -622,11 +642,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
         const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
         const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
         for (uint32_t p = lo; p < hi;) {
-            const Piece x = take_piece(a, s_line, 16u * NB, t, lo, hi, p);
+            const Piece x = take_piece(a, sq, s_line, 16u * NB, t, lo, hi, p);
             p += x.u1 - x.u0;
             Rows<DT, D, NB> w;
             w.begin(a, x, 0u, col, grp);
-            const uint32_t *const row_table = a.table + (uint64_t)x.r * a.stride;
+            const uint32_t *const row_table = sq.table + (uint64_t)x.r * a.stride;
             const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
             const uint32_t bmask = (1u << a.c.bshift) - 1u;
             const int32_t drafted = (int32_t)(x.total - x.ctx);
@@ -671,6 +691,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
                     const uint32_t bad = at.bad, un = min(u + WK, x.u1 - 1u);
                     at = step_at(a, head, ahead, x.total, err);
                     load_k(un, at);
+                    asm volatile("" ::: "memory");
                     ahead = step_pages(row_table, x, min(u + 2u * WK, x.u1 - 1u), a.c.bshift);
                     if (a.softcap > 0.0f)
                         cap_scores<NB>(a, s);
@@ -703,6 +724,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
                         }
                     }
                     load_v(un, at);
+                    asm volatile("" ::: "memory");  // requested here, not where they are used
                 }
             }
             end_piece<DT, D, NB, kAttWaves, WK>(a, x, w, c2, s_ml, s_o, wave);
@@ -717,11 +739,13 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
 // MFMA operands: two steps ahead into registers, then to one of two LDS
 // buffers, so that one barrier a step is enough.
 template <int DT, int D, int NB, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttArgs a, uint32_t n_tiles, Gate g)
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
 {
+    const Seqs sq = {q_start, table, lens, totals};
     constexpr uint32_t T = 64u * NW;
     constexpr uint32_t kRows = 16u * NB * NW;
     constexpr int KK = D / 32, DD = D / 16;
+    constexpr int VH = DD / 2;                               // V's operands at a time
     constexpr uint32_t kPieces = 8u * D;                     // of 16 bytes: K's, then V's
     constexpr uint32_t PER = (kPieces + T - 1u) / T;         // a thread's
     constexpr uint32_t kBuf = kPieces * 16u;
@@ -736,7 +760,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     const uint32_t col = lane & 15u, grp = lane >> 4;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
     uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line<T>(a, kRows, s_line, s_sum, pro_err); };
+    auto prologue = [&]() { plan_line<T>(a, sq, kRows, s_line, s_sum, pro_err); };
     const uint32_t bmask = (1u << a.c.bshift) - 1u;
     // piece j of this thread: which half of the step it lies in, its place in
     // the head's chunk, and what a token further is
@@ -753,11 +777,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
         const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
         const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
         for (uint32_t p = lo; p < hi;) {
-            const Piece x = take_piece(a, s_line, kRows, t, lo, hi, p);
+            const Piece x = take_piece(a, sq, s_line, kRows, t, lo, hi, p);
             p += x.u1 - x.u0;
             Rows<DT, D, NB> w;
             w.begin(a, x, x.row0 + 16u * NB * wave, col, grp);
-            const uint32_t *const row_table = a.table + (uint64_t)x.r * a.stride;
+            const uint32_t *const row_table = sq.table + (uint64_t)x.r * a.stride;
             const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
             const int32_t drafted = (int32_t)(x.total - x.ctx);
             u32x4 st[2][PER];
@@ -805,6 +829,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                 }
                 const uint8_t *const kb = buf + (grp * 32u + (col >> 2) * 8u + (col & 3u)) * 16u;
                 const uint8_t *const vb = buf + kBuf / 2u + (grp * D + col) * 16u;
+                // operands in groups, each requested while the one before is
+                // used, the first of V's before the softmax (left to itself the
+                // compiler waits for each operand in turn)
+                u32x4 kf[KK], vf[VH];
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    kf[kk] = *reinterpret_cast<const u32x4 *>(kb + kk * 2048);
+                __builtin_amdgcn_sched_barrier(0);
                 f32x4 s[NB][2];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
@@ -813,12 +845,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                         s[b][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk) {
-                        const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + q * 64);
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            s[b][q] = att_mfma<DT>(kf, w.q[b][kk], s[b][q]);
+                            s[b][q] = att_mfma<DT>(kf[kk], w.q[b][kk], s[b][q]);
+                        if (q == 0)
+                            kf[kk] = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + 64);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+#pragma unroll
+                for (int dd = 0; dd < VH; ++dd)
+                    vf[dd] = *reinterpret_cast<const u32x4 *>(vb + dd * 256);
+                __builtin_amdgcn_sched_barrier(0);
                 if (a.softcap > 0.0f)
                     cap_scores<NB>(a, s);
                 u32x4 pf[NB];
@@ -836,10 +874,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                 } else {
 #pragma unroll
                     for (int dd = 0; dd < DD; ++dd) {
-                        const u32x4 vf = *reinterpret_cast<const u32x4 *>(vb + dd * 256);
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            w.acc[b][dd] = att_mfma<DT>(vf, pf[b], w.acc[b][dd]);
+                            w.acc[b][dd] = att_mfma<DT>(vf[dd % VH], pf[b], w.acc[b][dd]);
+                        if (dd + VH < DD)
+                            vf[dd % VH] = *reinterpret_cast<const u32x4 *>(vb + (dd + VH) * 256);
                     }
                 }
             };
@@ -864,8 +903,9 @@ constexpr uint32_t kJoinRows = 4;  // rows of a join tile, one a wavefront
 // Joins the pieces of segments that lie in several ranges, a wavefront a row
 // (token and query head).  Segments inside one range were written whole.
 template <int DT, int D>
-__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t rb, uint32_t n_tiles, Gate g)
+__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, SGDRC_SEQS_ARGS, uint32_t rb, uint32_t n_tiles, Gate g)
 {
+    const Seqs sq = {q_start, table, lens, totals};
     constexpr uint32_t PER = (D + 63) / 64;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
@@ -873,7 +913,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
     const uint32_t lane = threadIdx.x & 63u;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
     uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line<kAttThreads>(a, rb, s_line, s_sum, pro_err); };
+    auto prologue = [&]() { plan_line<kAttThreads>(a, sq, rb, s_line, s_sum, pro_err); };
     auto body = [&](uint32_t t, uint32_t &) {
         const uint64_t i = (uint64_t)t * kJoinRows + wave;
         const uint32_t token = (uint32_t)(i / a.heads), qh = (uint32_t)(i % a.heads);
@@ -882,13 +922,13 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
         uint32_t rlo = 0u, rhi = a.n_requests;
         while (rhi - rlo > 1u) {
             const uint32_t mid = (rlo + rhi) >> 1;
-            if (a.q_start[mid] <= token)
+            if (sq.q_start[mid] <= token)
                 rlo = mid;
             else
                 rhi = mid;
         }
         const uint32_t r = __builtin_amdgcn_readfirstlane(rlo);
-        const Req rq = load_req(a, r);
+        const Req rq = load_req(a, sq, r);
         const bool mine = token < a.n_tokens && token >= rq.start && token - rq.start < rq.nodes && steps != 0u;
         const uint32_t node = token - rq.start;
         const uint32_t ranges = n_ranges(a, steps);
@@ -952,8 +992,9 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, uint32_t
 
 // -------------------------------------------------------------------- host
 
-typedef void (*AttKernel)(AttArgs, uint32_t, Gate);
-typedef void (*JoinKernel)(AttArgs, uint32_t, uint32_t, Gate);
+typedef void (*AttKernel)(AttArgs, const uint32_t *, const uint32_t *, const int32_t *, const int32_t *, uint32_t, Gate);
+typedef void (*JoinKernel)(AttArgs, const uint32_t *, const uint32_t *, const int32_t *, const int32_t *, uint32_t,
+                           uint32_t, Gate);
 
 // How a call's rows are spread, by the most rows a segment can have: the
 // kernel, its wavefronts, blocks of 16 rows of each, and the ranges that the
@@ -1109,10 +1150,6 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     a.o_token = o->token_stride * 2u;
     a.o_head = o->head_stride * 2u;
     a.lse = d_lse;
-    a.q_start = d_q_start;
-    a.table = blocks->table;
-    a.lens = d_lens;
-    a.totals = d_totals;
     a.mask = d_mask;
     a.work = static_cast<float *>(d_work);
     a.n_requests = blocks->n_requests;
@@ -1134,15 +1171,15 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     if ((rc = make_gate(c, stream, f.ranges, kStreamGroupCus, &g, &li, false, true)))
         return rc;
     const int threads = (int)(64u * f.waves);
-    hipLaunchKernelGGL(k, dim3(gated_grid(c, att_occupancy(k, threads), f.ranges, li)), dim3(threads), 0, s, a, f.ranges,
-                       g);
+    hipLaunchKernelGGL(k, dim3(gated_grid(c, att_occupancy(k, threads), f.ranges, li)), dim3(threads), 0, s, a, d_q_start,
+                       blocks->table, d_lens, d_totals, f.ranges, g);
     SGDRC_HIP(hipGetLastError());
     if ((rc = finish_static_tlog(g, s)))
         return rc;
     if ((rc = make_gate(c, stream, join_tiles, kStreamGroupCus, &g, &li, false, true)))
         return rc;
-    hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join, kAttThreads), join_tiles, li)), dim3(kAttThreads), 0, s, a, rb,
-                       (uint32_t)join_tiles, g);
+    hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join, kAttThreads), join_tiles, li)), dim3(kAttThreads), 0, s, a,
+                       d_q_start, blocks->table, d_lens, d_totals, rb, (uint32_t)join_tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);
 }
