@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "kv_common.hpp"
 
@@ -261,17 +262,44 @@ __device__ __forceinline__ float marked(float n, float n0)
     return k >> 12 || n0 != 0.0f ? NAN : v;
 }
 
-// The largest of a row's values over its four lanes.
+// Each lane's value and that of the lane 16 (32) away, in an order that both
+// see alike.
+struct Two {
+    float a, b;
+};
+
+// (the elements go through scalars: a bit cast of a vector's element takes the
+// first of them whichever is named)
+__device__ __forceinline__ Two swap16(float v)
+{
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const u32x2 t = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t t0 = t[0], t1 = t[1];
+    return {__builtin_bit_cast(float, t0), __builtin_bit_cast(float, t1)};
+}
+
+__device__ __forceinline__ Two swap32(float v)
+{
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const u32x2 t = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const uint32_t t0 = t[0], t1 = t[1];
+    return {__builtin_bit_cast(float, t0), __builtin_bit_cast(float, t1)};
+}
+
+// A row's four lanes are 16 apart: the values of the others arrive by swaps of
+// half and quarter wavefronts, on the vector ALUs.
 __device__ __forceinline__ float row_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    const Two p = swap16(v);
+    const Two q = swap32(fmaxf(p.a, p.b));
+    return fmaxf(q.a, q.b);
 }
 
 __device__ __forceinline__ float row_sum(float v)
 {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    const Two p = swap16(v);
+    const Two q = swap32(p.a + p.b);
+    return q.a + q.b;
 }
 
 // n low bits, n of any size.
@@ -374,7 +402,7 @@ __device__ __forceinline__ StepAt step_at(const AttArgs &a, const uint8_t *head,
     at.bad = 0u;
 #pragma unroll
     for (uint32_t i = 0; i < 2u; ++i) {
-        const bool bad = (uint64_t)s.e[i] >= a.c.pool_pages;
+        const bool bad = s.e[i] > (uint32_t)(a.c.pool_pages - 1u);
         at.bad |= bad || total == 0u ? 1u << i : 0u;
         err |= bad && total != 0u ? kDevErrPtRange : 0u;
         at.p[i] = head + ((uint64_t)(bad || total == 0u ? 0u : s.e[i]) << a.c.shift);
@@ -491,34 +519,32 @@ template <int DT, int D, int NB, typename LoadV>
 __device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[NB], const uint32_t (&seen)[NB],
                                         LoadV load_v)
 {
-    u32x4 some[NB], none[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b) {
+        u32x4 some, none;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const uint32_t sees = pair_mask(seen[b], w), weight = spread_top(top_from<1u>(pf[b][w]));
-            some[b][w] = sees & weight & kOne<DT>;
-            none[b][w] = sees & ~weight & kOne<DT>;
+            some[w] = sees & weight & kOne<DT>;
+            none[w] = sees & ~weight & kOne<DT>;
         }
 #pragma unroll
-    for (int dd = 0; dd < D / 16; ++dd) {
-        u32x4 v = load_v(dd), marks;
+        for (int dd = 0; dd < D / 16; ++dd) {
+            u32x4 v = load_v(dd), marks;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t two = v[w];
-            marks[w] = take_marks<DT>(two);
-            v[w] = two;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
+            for (int w = 0; w < 4; ++w) {
+                uint32_t two = v[w];
+                marks[w] = take_marks<DT>(two);
+                v[w] = two;
+            }
             const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
             r.acc[b][dd] = att_mfma<DT>(v, pf[b], r.acc[b][dd]);
-            const f32x4 n = att_mfma<DT>(marks, some[b], z), n0 = att_mfma<DT>(marks, none[b], z);
+            const f32x4 n = att_mfma<DT>(marks, some, z), n0 = att_mfma<DT>(marks, none, z);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 r.acc[b][dd][i] += marked(n[i], n0[i]);
+            __builtin_amdgcn_sched_barrier(0);  // one block's marks at a time
         }
-        __builtin_amdgcn_sched_barrier(0);  // one block's marks at a time
     }
 }
 
@@ -536,81 +562,40 @@ __device__ __forceinline__ uint32_t keep_there(u32x4 &v, uint32_t there)
     return odd;
 }
 
-// The end of a piece: joins the WK wavefronts that shared rows (maxima and
-// sums first, then the weighted V, 16 rows at a time) and writes the rows, or
-// the partial result.  NW wavefronts; wavefront ``wave`` has rows 16 NB (wave
-// / WK) .. of the segment.  Ends with a barrier.
-template <int DT, int D, int NB, uint32_t NW, uint32_t WK>
-__device__ __forceinline__ void end_piece(const AttArgs &a, const Piece &x, Rows<DT, D, NB> &w, float c2,
-                                          float (*s_ml)[16 * NB][2], float (*s_o)[16][D + 4], uint32_t wave)
+// A row's result, or its part of one, 4 dims from d on.
+template <int DT, int D>
+__device__ __forceinline__ void put_row(const AttArgs &a, const Piece &x, uint32_t rb, uint32_t in, uint32_t d, f32x4 v)
 {
-    constexpr uint32_t kRows = 16u * NB * NW / WK;
-    const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, grp = lane >> 4;
-    const uint32_t wq = wave / WK;
-    float f[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        w.l[b] = row_sum(w.l[b]);
-        if (grp == 0u) {
-            s_ml[wave][16 * b + col][0] = w.m[b];
-            s_ml[wave][16 * b + col][1] = w.l[b];
+    const uint32_t row = x.row0 + in;
+    if (row >= x.rows)
+        return;
+    if (x.whole) {
+        uint8_t *const op = a.o + (x.start + row / a.group) * a.o_token + (x.h * a.group + row % a.group) * a.o_head + d * 2u;
+        const u32x2 two = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+        *reinterpret_cast<u32x2 *>(op) = two;
+    } else {
+        *reinterpret_cast<f32x4 *>(part_rows(a.work, x.part, rb, D) + (uint64_t)in * D + d) = v;
+    }
+}
+
+// A row's maximum and sum: to the workspace, or as its log-sum-exp.  Returns
+// what its weighted V is to be multiplied with.
+template <int DT, int D>
+__device__ __forceinline__ float put_stats(const AttArgs &a, const Piece &x, uint32_t rb, uint32_t in, float m, float l,
+                                           float c2, bool write)
+{
+    if (write && x.row0 + in < x.rows) {
+        if (!x.whole) {
+            float *const st = part_stats(a.work, x.part, rb, D) + in * 2u;
+            st[0] = m;
+            st[1] = l;
+        } else if (a.lse) {
+            const uint32_t row = x.row0 + in;
+            a.lse[(uint64_t)(x.start + row / a.group) * a.heads + x.h * a.group + row % a.group] =
+                l == 0.0f ? -INFINITY : (m * c2 - kLift<DT> + __log2f(l)) * kLn2;
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        float mj = -INFINITY;
-#pragma unroll
-        for (uint32_t k = 0; k < WK; ++k)
-            mj = fmaxf(mj, s_ml[wq * WK + k][16 * b + col][0]);
-        const float use = mj == -INFINITY ? 0.0f : mj;
-        float lj = 0.0f;
-#pragma unroll
-        for (uint32_t k = 0; k < WK; ++k)
-            lj += s_ml[wq * WK + k][16 * b + col][1] *
-                  __builtin_amdgcn_exp2f((s_ml[wq * WK + k][16 * b + col][0] - use) * c2);
-        f[b] = __builtin_amdgcn_exp2f((w.m[b] - use) * c2);
-        if (x.whole)
-            f[b] = lj > 0.0f ? f[b] / lj : lj == 0.0f ? 0.0f : lj;  // NaN stays NaN
-        const uint32_t in = 16u * (wq * NB + b) + col;
-        if (wave % WK == 0u && grp == 0u && x.row0 + in < x.rows) {
-            if (!x.whole) {
-                float *const st = part_stats(a.work, x.part, kRows, D) + in * 2u;
-                st[0] = mj;
-                st[1] = lj;
-            } else if (a.lse) {
-                a.lse[(uint64_t)w.tok[b] * a.heads + x.h * a.group + (x.row0 + in) % a.group] =
-                    lj == 0.0f ? -INFINITY : (mj * c2 - kLift<DT> + __log2f(lj)) * kLn2;
-            }
-        }
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int dd = 0; dd < D / 16; ++dd)
-            *reinterpret_cast<f32x4 *>(&s_o[wave][col][dd * 16 + grp * 4u]) = w.acc[b][dd] * f[b];
-        __syncthreads();
-        // each group of WK wavefronts adds up its own 16 rows, 4 dims a thread
-        for (uint32_t i = threadIdx.x % (64u * WK); i < 16u * (D / 4); i += 64u * WK) {
-            const uint32_t rr = i / (D / 4), d = i % (D / 4) * 4u;
-            const uint32_t in = 16u * (wq * NB + b) + rr, row = x.row0 + in;
-            f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[wq * WK][rr][d]);
-#pragma unroll
-            for (uint32_t k = 1; k < WK; ++k)
-                v += *reinterpret_cast<const f32x4 *>(&s_o[wq * WK + k][rr][d]);
-            if (row < x.rows) {
-                if (x.whole) {
-                    uint8_t *const op = a.o + (x.start + row / a.group) * a.o_token +
-                                        (x.h * a.group + row % a.group) * a.o_head + d * 2u;
-                    const u32x2 two = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
-                    *reinterpret_cast<u32x2 *>(op) = two;
-                } else {
-                    *reinterpret_cast<f32x4 *>(part_rows(a.work, x.part, kRows, D) + (uint64_t)in * D + d) = v;
-                }
-            }
-        }
-        __syncthreads();
-    }
+    return !x.whole ? 1.0f : l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // NaN stays NaN
 }
 
 // Few rows (16 NB of a segment at most): bound by the cache's bytes.  The four
@@ -660,15 +645,15 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
                 const uint8_t *const kp = (col < 8u ? at.p[0] : at.p[1]) + k_lane + (u * kStep & bmask) * 16u;
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) {
-                    kf[0][kk] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)kk * 64u << a.c.bshift));
-                    kf[1][kk] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)kk * 64u << a.c.bshift) + 64u);
+                    kf[0][kk] = load_nt(kp + ((uint32_t)kk * 64u << a.c.bshift));
+                    kf[1][kk] = load_nt(kp + ((uint32_t)kk * 64u << a.c.bshift) + 64u);
                 }
             };
             auto load_v = [&](uint32_t u, const StepAt &at) __attribute__((always_inline)) {
                 const uint8_t *const vp = (grp < 2u ? at.p[0] : at.p[1]) + v_lane + (u * kStep & bmask) * (2u * D);
 #pragma unroll
                 for (int dd = 0; dd < DD; ++dd)
-                    vf[dd] = *reinterpret_cast<const u32x4 *>(vp + dd * 256);
+                    vf[dd] = load_nt(vp + dd * 256);
             };
             uint32_t u = x.u0 + wave;
             if (u < x.u1) {
@@ -676,8 +661,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
                 load_k(u, at);
                 load_v(u, at);
                 StepPages ahead = step_pages(row_table, x, min(u + WK, x.u1 - 1u), a.c.bshift);
-                for (; u < x.u1; u += WK) {
-                    f32x4 s[NB][2];
+                auto scores = [&](f32x4 (&s)[NB][2]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -687,50 +671,114 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
                             for (int kk = 0; kk < KK; ++kk)
                                 s[b][q] = att_mfma<DT>(kf[q][kk], w.q[b][kk], s[b][q]);
                         }
-                    // the next step; past the piece's end its last one again
-                    const uint32_t bad = at.bad, un = min(u + WK, x.u1 - 1u);
+                };
+                // K of the next step (past the piece's end its last one again),
+                // which becomes ``at``
+                auto next_k = [&]() __attribute__((always_inline)) {
                     at = step_at(a, head, ahead, x.total, err);
-                    load_k(un, at);
-                    asm volatile("" ::: "memory");
+                    load_k(min(u + WK, x.u1 - 1u), at);
+                    asm volatile("" ::: "memory");  // requested here, not where they are used
                     ahead = step_pages(row_table, x, min(u + 2u * WK, x.u1 - 1u), a.c.bshift);
+                };
+                auto next_v = [&]() __attribute__((always_inline)) {
+                    load_v(min(u + WK, x.u1 - 1u), at);
+                    asm volatile("" ::: "memory");
+                };
+                auto products = [&](const u32x4 (&pf)[NB]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int dd = 0; dd < DD; ++dd)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
+                };
+                // steps that every row sees whole, in a loop of their own: with
+                // the others' code in it the compiler copies the accumulators
+                // every time
+                const uint32_t seen_steps = min(x.u1, x.ctx / kStep);
+                for (; u < seen_steps && at.bad == 0u; u += WK) {
+                    f32x4 s[NB][2];
+                    u32x4 pf[NB];
+                    scores(s);
+                    next_k();
                     if (a.softcap > 0.0f)
                         cap_scores<NB>(a, s);
+                    weigh<DT, D, NB>(w, s, c2, pf);
+                    products(pf);
+                    next_v();
+                }
+                for (; u < x.u1; u += WK) {
+                    f32x4 s[NB][2];
                     u32x4 pf[NB];
-                    if (u * kStep + kStep <= x.ctx && bad == 0u) {
-                        weigh<DT, D, NB>(w, s, c2, pf);
+                    uint32_t seen[NB];
+                    scores(s);
+                    const uint32_t bad = at.bad;
+                    next_k();
+                    if (a.softcap > 0.0f)
+                        cap_scores<NB>(a, s);
+                    const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
+                    const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
+                    uint32_t odd = 0u;
 #pragma unroll
-                        for (int dd = 0; dd < DD; ++dd)
-#pragma unroll
-                            for (int b = 0; b < NB; ++b)
-                                w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
-                    } else {
-                        const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
-                        const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
-                        uint32_t odd = 0u;
-#pragma unroll
-                        for (int dd = 0; dd < DD; ++dd)
-                            odd |= keep_there<DT>(vf[dd], there);
-                        uint32_t seen[NB];
-                        mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
-                        weigh<DT, D, NB>(w, s, c2, pf);
-                        if (__ballot(odd != 0u) != 0ull) {
-                            add_odd<DT, D, NB>(w, pf, seen, [&](int dd) { return vf[dd]; });
-                        } else {
-#pragma unroll
-                            for (int dd = 0; dd < DD; ++dd)
-#pragma unroll
-                                for (int b = 0; b < NB; ++b)
-                                    w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
-                        }
-                    }
-                    load_v(un, at);
-                    asm volatile("" ::: "memory");  // requested here, not where they are used
+                    for (int dd = 0; dd < DD; ++dd)
+                        odd |= keep_there<DT>(vf[dd], there);
+                    mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
+                    weigh<DT, D, NB>(w, s, c2, pf);
+                    if (__ballot(odd != 0u) != 0ull)
+                        add_odd<DT, D, NB>(w, pf, seen, [&](int dd) { return vf[dd]; });
+                    else
+                        products(pf);
+                    next_v();
                 }
             }
-            end_piece<DT, D, NB, kAttWaves, WK>(a, x, w, c2, s_ml, s_o, wave);
+            // Join the wavefronts: maxima and sums first, then the weighted V,
+            // 16 rows at a time.
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                w.l[b] = row_sum(w.l[b]);
+                if (grp == 0u) {
+                    s_ml[wave][16 * b + col][0] = w.m[b];
+                    s_ml[wave][16 * b + col][1] = w.l[b];
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float m = -INFINITY, l = 0.0f;
+#pragma unroll
+                for (uint32_t k = 0; k < WK; ++k)
+                    m = fmaxf(m, s_ml[k][16 * b + col][0]);
+                const float use = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (uint32_t k = 0; k < WK; ++k)
+                    l += s_ml[k][16 * b + col][1] * __builtin_amdgcn_exp2f((s_ml[k][16 * b + col][0] - use) * c2);
+                const float f = __builtin_amdgcn_exp2f((w.m[b] - use) * c2) *
+                                put_stats<DT, D>(a, x, 16u * NB, 16u * b + col, m, l, c2, wave == 0u && grp == 0u);
+#pragma unroll
+                for (int dd = 0; dd < DD; ++dd)
+                    *reinterpret_cast<f32x4 *>(&s_o[wave][col][dd * 16 + grp * 4u]) = w.acc[b][dd] * f;
+                __syncthreads();
+                for (uint32_t i = threadIdx.x; i < 16u * (D / 4); i += kAttThreads) {
+                    const uint32_t rr = i / (D / 4), d = i % (D / 4) * 4u;
+                    f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[0][rr][d]);
+#pragma unroll
+                    for (uint32_t k = 1; k < WK; ++k)
+                        v += *reinterpret_cast<const f32x4 *>(&s_o[k][rr][d]);
+                    put_row<DT, D>(a, x, 16u * NB, 16u * b + rr, d, v);
+                }
+                __syncthreads();
+            }
         }
     };
     single_tile_loop(g, n_tiles, prologue, body);
+}
+
+// The token of a step that lies at place ``p`` of K's LDS: the two K tiles' rows
+// one after the other, so that the sixteen lanes that read a tile's rows of one
+// 16-byte column meet all banks (in the order of memory every second lane's
+// bank is taken twice).
+__device__ __forceinline__ uint32_t lds_token(uint32_t p)
+{
+    return (p >> 2 & 3u) * 8u + (p >> 4 & 1u) * 4u + (p & 3u);
 }
 
 // Many rows: NW wavefronts of 16 NB rows each take the same steps, whose K and
@@ -749,12 +797,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     constexpr uint32_t kPieces = 8u * D;                     // of 16 bytes: K's, then V's
     constexpr uint32_t PER = (kPieces + T - 1u) / T;         // a thread's
     constexpr uint32_t kBuf = kPieces * 16u;
-    constexpr uint32_t kOut = NW * 16u * (D + 4u) * 4u;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[NW];
-    __shared__ float s_ml[NW][16 * NB][2];
-    // two steps, and at a piece's end the rows' results
-    __shared__ __attribute__((aligned(16))) uint8_t s_kv[2u * kBuf > kOut ? 2u * kBuf : kOut];
+    __shared__ __attribute__((aligned(16))) uint8_t s_kv[2u * kBuf];  // two steps
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t col = lane & 15u, grp = lane >> 4;
@@ -764,9 +809,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     const uint32_t bmask = (1u << a.c.bshift) - 1u;
     // piece j of this thread: which half of the step it lies in, its place in
     // the head's chunk, and what a token further is
-    auto half_of = [&](uint32_t i) { return (i < kPieces / 2u ? i % 32u >> 4 : (i - kPieces / 2u) / D >> 1); };
+    auto half_of = [&](uint32_t i) { return (i < kPieces / 2u ? lds_token(i) >> 4 : (i - kPieces / 2u) / D >> 1); };
     auto place_of = [&](uint32_t i) {
-        return i < kPieces / 2u ? k_off<D>(i / 32u, i % 32u & bmask, a.c.bshift)
+        return i < kPieces / 2u ? k_off<D>(i / 32u, lds_token(i) & bmask, a.c.bshift)
                                 : v_off<D>(((i - kPieces / 2u) / D * 8u & bmask) >> 3, i % D, a.c.bshift);
     };
     static_assert((kPieces / 2u) % D == 0u && kPieces / 2u % 32u == 0u, "V's pieces begin a row");
@@ -798,11 +843,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                             (half_of(i) ? at.p[1] : at.p[0]) + place_of(i) + off * (i < kPieces / 2u ? 16u : 2u * D));
                 }
             };
-            auto step = [&](uint32_t u, u32x4 (&from)[PER], uint32_t &bad_of, uint8_t *buf, StepPages &ahead) __attribute__((always_inline)) {
+            // ``edge``: a step that some row does not see whole
+            auto step = [&](auto edge, uint32_t u, u32x4 (&from)[PER], uint32_t &bad_of, uint8_t *buf,
+                            StepPages &ahead) __attribute__((always_inline)) {
                 const uint32_t bad = bad_of;
-                const bool edge = u * kStep + kStep > x.ctx || bad != 0u;
                 uint32_t odd = 0u;
-                if (edge) {
+                if constexpr (edge) {
 #pragma unroll
                     for (uint32_t j = 0; j < PER; ++j) {
                         const uint32_t i = j * T + threadIdx.x;
@@ -819,15 +865,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                     if (kPieces % T == 0u || i < kPieces)
                         *reinterpret_cast<u32x4 *>(buf + i * 16u) = from[j];
                 }
-                if (edge)
-                    odd = (uint32_t)__syncthreads_or((int)(odd != 0u));
+                if constexpr (edge)
+                    odd = __builtin_amdgcn_readfirstlane((uint32_t)__syncthreads_or((int)(odd != 0u)));
                 else
                     __syncthreads();
-                if (u + 2u < x.u1) {
-                    fetch(u + 2u, ahead, from, bad_of);
-                    ahead = step_pages(row_table, x, min(u + 3u, x.u1 - 1u), a.c.bshift);
-                }
-                const uint8_t *const kb = buf + (grp * 32u + (col >> 2) * 8u + (col & 3u)) * 16u;
+                // past the piece's end its last step again: where loads may or may
+                // not have been made, the compiler has to wait for all of them
+                // before it uses older ones
+                fetch(min(u + 2u, x.u1 - 1u), ahead, from, bad_of);
+                ahead = step_pages(row_table, x, min(u + 3u, x.u1 - 1u), a.c.bshift);
+                const uint8_t *const kb = buf + (grp * 32u + col) * 16u;
                 const uint8_t *const vb = buf + kBuf / 2u + (grp * D + col) * 16u;
                 // operands in groups, each requested while the one before is
                 // used, the first of V's before the softmax (left to itself the
@@ -849,7 +896,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                         for (int b = 0; b < NB; ++b)
                             s[b][q] = att_mfma<DT>(kf[kk], w.q[b][kk], s[b][q]);
                         if (q == 0)
-                            kf[kk] = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + 64);
+                            kf[kk] = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + 256);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -861,13 +908,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                     cap_scores<NB>(a, s);
                 u32x4 pf[NB];
                 uint32_t seen[NB];
-                if (edge) {
+                if constexpr (edge) {
                     const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
                     const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
                     mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
                 }
                 weigh<DT, D, NB>(w, s, c2, pf);
-                if (odd != 0u) {
+                if (edge && odd != 0u) {
                     add_odd<DT, D, NB>(w, pf, seen, [&](int dd) {
                         return *reinterpret_cast<const u32x4 *>(vb + dd * 256);
                     });
@@ -886,13 +933,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
             fetch(min(x.u0 + 1u, x.u1 - 1u), step_pages(row_table, x, min(x.u0 + 1u, x.u1 - 1u), a.c.bshift), st[1],
                   bads[1]);
             StepPages ahead = step_pages(row_table, x, min(x.u0 + 2u, x.u1 - 1u), a.c.bshift);
-            for (uint32_t u = x.u0; u < x.u1; u += 2u) {
-                step(u, st[0], bads[0], s_kv, ahead);
-                if (u + 1u < x.u1)
-                    step(u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
+            // steps that every row sees whole in a loop of their own, two at a
+            // time: with the others' code in it the compiler copies the
+            // accumulators every time
+            const uint32_t seen_steps = min(x.u1, x.ctx / kStep);
+            uint32_t u = x.u0;
+            for (; u + 2u <= seen_steps && (bads[0] | bads[1]) == 0u; u += 2u) {
+                step(std::false_type(), u, st[0], bads[0], s_kv, ahead);
+                step(std::false_type(), u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
             }
-            __syncthreads();  // the last step is read: its LDS becomes the results'
-            end_piece<DT, D, NB, NW, 1>(a, x, w, c2, s_ml, reinterpret_cast<float(*)[16][D + 4]>(s_kv), wave);
+            for (; u < x.u1; u += 2u) {
+                step(std::true_type(), u, st[0], bads[0], s_kv, ahead);
+                if (u + 1u < x.u1)
+                    step(std::true_type(), u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t in = 16u * (NB * wave + b) + col;
+                const float f = put_stats<DT, D>(a, x, kRows, in, w.m[b], row_sum(w.l[b]), c2, grp == 0u);
+#pragma unroll
+                for (int dd = 0; dd < DD; ++dd)
+                    put_row<DT, D>(a, x, kRows, in, dd * 16u + grp * 4u, w.acc[b][dd] * f);
+            }
+            __syncthreads();  // the last step is read
         }
     };
     single_tile_loop(g, n_tiles, prologue, body);

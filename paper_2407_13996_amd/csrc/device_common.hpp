@@ -742,7 +742,9 @@ __device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles
             if (allowed)
                 tile = claim_ticket(&g.q->grp_next[0], &s_ticket);
             if (tile >= n_tiles) {
-                if (!arrive_last(g, &s_flag))
+                // (the flag is the same in every lane; without saying so here all
+                // that follows, the body's scalars too, would count as per-lane)
+                if (__builtin_amdgcn_readfirstlane(arrive_last(g, &s_flag) ? 1u : 0u) == 0u)
                     break;
                 t = __builtin_amdgcn_readfirstlane(
                     __hip_atomic_load(&g.q->grp_next[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
@@ -758,7 +760,7 @@ __device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles
             t += from == kStride ? workers : 1u;
         }
         log_tile(g, cu, tile);
-        body(tile, err);
+        body(__builtin_amdgcn_readfirstlane(tile), err);
     }
     if (from == kLeft) {
         reset_slot(g.q);
