@@ -133,34 +133,46 @@ __device__ __forceinline__ void plan_line(const AttArgs &a, const Seqs &sq, uint
     for (uint32_t w = 0; w < wave; ++w)
         run += s_sum[w];
     for (uint32_t r = r0; r < r1; ++r) {
-        const Req q = load_req(a, sq, r);
         s_line[r] = run;
-        run += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
+        if (per == 1u) {
+            run += sum;
+        } else {
+            const Req q = load_req(a, sq, r);
+            run += q.nodes ? seg_steps(q) * row_blocks(q, a.group, rb) * a.c.heads : 0u;
+        }
         if (r == R - 1u)
             s_line[R] = run;
     }
     __syncthreads();
 }
 
-// The cut of a line of ``steps`` into ranges: range t is [cut(t), cut(t + 1)).
-__device__ __forceinline__ uint32_t n_ranges(const AttArgs &a, uint32_t steps)
-{
-    return min(a.most_ranges, (steps + kMinSteps - 1u) / kMinSteps);
-}
+// The cut of a line of steps into ranges of almost equal length: range t is
+// [cut(t), cut(t + 1)), cut(t) = t steps / ranges, by 32-bit divisions.
+struct Cuts {
+    uint32_t steps, n, whole, rest;
 
-__device__ __forceinline__ uint32_t range_cut(uint32_t t, uint32_t steps, uint32_t ranges)
-{
-    return (uint32_t)((uint64_t)t * steps / ranges);
-}
+    __device__ __forceinline__ Cuts(const AttArgs &a, uint32_t line)
+    {
+        steps = __builtin_amdgcn_readfirstlane(line);
+        n = min(a.most_ranges, (steps + kMinSteps - 1u) / kMinSteps);
+        whole = steps / max(n, 1u);
+        rest = steps - whole * n;
+    }
 
-// The range that step ``p`` is in.
-__device__ __forceinline__ uint32_t range_of(uint32_t p, uint32_t steps, uint32_t ranges)
-{
-    uint32_t t = (uint32_t)(((uint64_t)p * ranges) / steps);
-    while (t + 1u < ranges && range_cut(t + 1u, steps, ranges) <= p)
-        ++t;
-    return t;
-}
+    __device__ __forceinline__ uint32_t cut(uint32_t t) const { return t * whole + t * rest / max(n, 1u); }
+
+    // the range that step ``p`` is in (ranges are at most 512, so that the
+    // estimate is at most one off)
+    __device__ __forceinline__ uint32_t range_of(uint32_t p) const
+    {
+        uint32_t t = min((uint32_t)((float)p * ((float)n / (float)steps)), n - 1u);
+        if (t && cut(t) > p)
+            --t;
+        else if (t + 1u < n && cut(t + 1u) <= p)
+            ++t;
+        return t;
+    }
+};
 
 // The last request that begins at or before step ``p`` and has any.
 __device__ __forceinline__ uint32_t find_request(const uint32_t *s_line, uint32_t R, uint32_t p)
@@ -622,10 +634,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
     auto prologue = [&]() { plan_line<kAttThreads>(a, sq, 16u * NB, s_line, s_sum, pro_err); };
     auto body = [&](uint32_t t, uint32_t &err) {
         err |= pro_err;
-        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
-        const uint32_t ranges = n_ranges(a, steps);
-        const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
-        const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
+        const Cuts cuts(a, s_line[a.n_requests]);
+        const uint32_t lo = t < cuts.n ? cuts.cut(t) : 0u;
+        const uint32_t hi = t < cuts.n ? cuts.cut(t + 1u) : 0u;
         for (uint32_t p = lo; p < hi;) {
             const Piece x = take_piece(a, sq, s_line, 16u * NB, t, lo, hi, p);
             p += x.u1 - x.u0;
@@ -817,10 +828,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     static_assert((kPieces / 2u) % D == 0u && kPieces / 2u % 32u == 0u, "V's pieces begin a row");
     auto body = [&](uint32_t t, uint32_t &err) {
         err |= pro_err;
-        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
-        const uint32_t ranges = n_ranges(a, steps);
-        const uint32_t lo = t < ranges ? range_cut(t, steps, ranges) : 0u;
-        const uint32_t hi = t < ranges ? range_cut(t + 1u, steps, ranges) : 0u;
+        const Cuts cuts(a, s_line[a.n_requests]);
+        const uint32_t lo = t < cuts.n ? cuts.cut(t) : 0u;
+        const uint32_t hi = t < cuts.n ? cuts.cut(t + 1u) : 0u;
         for (uint32_t p = lo; p < hi;) {
             const Piece x = take_piece(a, sq, s_line, kRows, t, lo, hi, p);
             p += x.u1 - x.u0;
@@ -961,94 +971,125 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     single_tile_loop(g, n_tiles, prologue, body);
 }
 
-constexpr uint32_t kJoinRows = 4;  // rows of a join tile, one a wavefront
+// Lanes of a join's row (16 bytes each of the first D / 4), and rows of a tile.
+constexpr uint32_t join_lanes(uint32_t dim) { return dim <= 64u ? 16u : dim <= 128u ? 32u : 64u; }
+constexpr uint32_t join_rows(uint32_t dim) { return kAttThreads / join_lanes(dim); }
 
-// Joins the pieces of segments that lie in several ranges, a wavefront a row
-// (token and query head).  Segments inside one range were written whole.
+// A segment that lies in several ranges, t0 to t1: its rows, of head ``h``.
+struct CutSegment {
+    uint32_t start, rows, row0, h, t0, t1;
+};
+
+constexpr uint32_t kMostRanges = 512;
+
+// Joins the pieces of segments that lie in several ranges; those inside one
+// were written whole.  Every workgroup first lists those segments, a cut
+// between ranges a thread, the first cut of a segment having it; a tile is
+// some rows of one of them.  (Tiles by rows of the output, each with its
+// request and cuts to find, took 88 us for 64 requests of 24 nodes and 17 for
+// one long cache, where these take 25 and 11.)
+// Bound by latency: a row's pieces are asked for eight at a time.
 template <int DT, int D>
-__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, SGDRC_SEQS_ARGS, uint32_t rb, uint32_t n_tiles, Gate g)
+__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, SGDRC_SEQS_ARGS, uint32_t rb, uint32_t chunks,
+                                                             uint32_t n_tiles, Gate g)
 {
     const Seqs sq = {q_start, table, lens, totals};
-    constexpr uint32_t PER = (D + 63) / 64;
+    constexpr uint32_t LANES = join_lanes(D), AHEAD = 8;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t lane = threadIdx.x & 63u;
+    __shared__ CutSegment s_cut[kMostRanges];
+    const uint32_t lane = threadIdx.x % LANES, d = lane * 4u;
     const float c2 = a.softcap > 0.0f ? 1.0f : a.scale * kLog2e;
-    uint32_t pro_err = 0u;
-    auto prologue = [&]() { plan_line<kAttThreads>(a, sq, rb, s_line, s_sum, pro_err); };
-    auto body = [&](uint32_t t, uint32_t &) {
-        const uint64_t i = (uint64_t)t * kJoinRows + wave;
-        const uint32_t token = (uint32_t)(i / a.heads), qh = (uint32_t)(i % a.heads);
-        const uint32_t steps = __builtin_amdgcn_readfirstlane(s_line[a.n_requests]);
-        // the last request whose rows begin at or before the token
-        uint32_t rlo = 0u, rhi = a.n_requests;
-        while (rhi - rlo > 1u) {
-            const uint32_t mid = (rlo + rhi) >> 1;
-            if (sq.q_start[mid] <= token)
-                rlo = mid;
-            else
-                rhi = mid;
-        }
-        const uint32_t r = __builtin_amdgcn_readfirstlane(rlo);
-        const Req rq = load_req(a, sq, r);
-        const bool mine = token < a.n_tokens && token >= rq.start && token - rq.start < rq.nodes && steps != 0u;
-        const uint32_t node = token - rq.start;
-        const uint32_t ranges = n_ranges(a, steps);
-        uint32_t t0 = 0u, t1 = 0u, in = 0u, seg0 = 0u;
-        if (mine) {
-            const uint32_t row = node * a.group + qh % a.group;
-            const uint32_t U = seg_steps(rq), blocks = row_blocks(rq, a.group, rb);
-            seg0 = s_line[r] + (qh / a.group * blocks + row / rb) * U;
-            in = row % rb;
-            t0 = range_of(seg0, steps, ranges);
-            t1 = range_of(seg0 + U - 1u, steps, ranges);
-        }
-        if (t0 < t1) {
-            // a segment's first piece is its range's last, the others their range's first
-            float mx = -INFINITY;
-            for (uint32_t q = t0 + lane; q <= t1; q += 64u)
-                mx = fmaxf(mx, part_stats(a.work, 2u * q + (q == t0 ? 1u : 0u), rb, D)[in * 2u]);
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1)
-                mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-            const float use = mx == -INFINITY ? 0.0f : mx;
-            float l = 0.0f, v[PER];
-#pragma unroll
-            for (uint32_t e = 0; e < PER; ++e)
-                v[e] = 0.0f;
-            for (uint32_t q0 = t0; q0 <= t1; q0 += 64u) {
-                const uint32_t q = q0 + lane;
-                float f = 0.0f;
-                if (q <= t1) {
-                    const float *const st = part_stats(a.work, 2u * q + (q == t0 ? 1u : 0u), rb, D) + in * 2u;
-                    f = __builtin_amdgcn_exp2f((st[0] - use) * c2);
-                    l += st[1] * f;
-                }
-                const uint32_t n = min(t1 + 1u - q0, 64u);
-                for (uint32_t k = 0; k < n; ++k) {
-                    const uint32_t qq = q0 + k;
-                    const float w = __shfl(f, (int)k, 64);
-                    const float *const src = part_rows(a.work, 2u * qq + (qq == t0 ? 1u : 0u), rb, D) + (uint64_t)in * D;
-#pragma unroll
-                    for (uint32_t e = 0; e < PER; ++e)
-                        if (lane + 64u * e < (uint32_t)D)
-                            v[e] += src[lane + 64u * e] * w;
-                }
+    uint32_t n_cut = 0u;
+    auto prologue = [&]() {
+        uint32_t seen_err = 0u;  // raised by the kernel before
+        plan_line<kAttThreads>(a, sq, rb, s_line, s_sum, seen_err);
+        const Cuts cuts(a, s_line[a.n_requests]);
+        for (uint32_t t0 = 0u; t0 + 1u < cuts.n; t0 += kAttThreads) {
+            const uint32_t t = t0 + threadIdx.x + 1u;
+            bool first = false;
+            CutSegment c = {};
+            if (t < cuts.n) {
+                const uint32_t p = cuts.cut(t), r = find_request(s_line, a.n_requests, p);
+                const Req rq = load_req(a, sq, r);
+                const uint32_t U = seg_steps(rq), k = (p - s_line[r]) / U, seg0 = s_line[r] + k * U;
+                const uint32_t blocks = row_blocks(rq, a.group, rb);
+                first = p != seg0 && cuts.cut(t - 1u) <= seg0;
+                c = {rq.start, rq.nodes * a.group, k % blocks * rb, k / blocks, t - 1u, cuts.range_of(seg0 + U - 1u)};
             }
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1)
-                l += __shfl_xor(l, off, 64);
-            const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-            uint8_t *const op = a.o + token * a.o_token + qh * a.o_head;
-#pragma unroll
-            for (uint32_t e = 0; e < PER; ++e)
-                if (lane + 64u * e < (uint32_t)D)
-                    *reinterpret_cast<uint16_t *>(op + (lane + 64u * e) * 2u) = (uint16_t)pack2<DT>(v[e] * inv, 0.0f);
-            if (a.lse && lane == 0u)
-                a.lse[(uint64_t)token * a.heads + qh] =
-                    l == 0.0f ? -INFINITY : (mx * c2 - kLift<DT> + __log2f(l)) * kLn2;
+            const uint64_t who = __ballot(first);
+            if ((threadIdx.x & 63u) == 0u)
+                s_sum[threadIdx.x >> 6] = (uint32_t)__popcll(who);
+            __syncthreads();
+            uint32_t at = n_cut + (uint32_t)__popcll(who & ((1ull << (threadIdx.x & 63u)) - 1ull));
+            for (uint32_t w = 0; w < kAttWaves; ++w) {
+                at += w < threadIdx.x >> 6 ? s_sum[w] : 0u;
+                n_cut += s_sum[w];
+            }
+            if (first)
+                s_cut[at] = c;
+            __syncthreads();
         }
+        n_cut = __builtin_amdgcn_readfirstlane(n_cut);
+    };
+    auto body = [&](uint32_t tile, uint32_t &) {
+        const uint32_t i = tile / chunks, in = tile % chunks * join_rows(D) + threadIdx.x / LANES;
+        if (i >= n_cut)
+            return;
+        const uint32_t row0 = s_cut[i].row0, row = row0 + in, h = s_cut[i].h, start = s_cut[i].start;
+        if (row >= s_cut[i].rows || in >= rb)
+            return;
+        // a segment's first piece is its range's last, the others their range's first
+        const uint32_t t0 = __builtin_amdgcn_readfirstlane(s_cut[i].t0), t1 = __builtin_amdgcn_readfirstlane(s_cut[i].t1);
+        auto part_of = [&](uint32_t q) { return 2u * q + (q == t0 ? 1u : 0u); };
+        // maximum and sum, so far
+        float m = -INFINITY, l = 0.0f;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t q0 = t0; q0 <= t1; q0 += LANES) {
+            const uint32_t q = min(q0 + lane, t1), n = min(t1 + 1u - q0, LANES);
+            f32x4 x[AHEAD];
+            auto load = [&](uint32_t k0) __attribute__((always_inline)) {
+#pragma unroll
+                for (uint32_t e = 0; e < AHEAD; ++e) {
+                    x[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    if (k0 + e < n && d < (uint32_t)D)
+                        x[e] = *reinterpret_cast<const f32x4 *>(part_rows(a.work, part_of(q0 + k0 + e), rb, D) +
+                                                                (uint64_t)in * D + d);
+                }
+                asm volatile("" ::: "memory");
+            };
+            const f32x2 st = *reinterpret_cast<const f32x2 *>(part_stats(a.work, part_of(q), rb, D) + in * 2u);
+            load(0u);
+            float mx = fmaxf(m, st[0]);
+#pragma unroll
+            for (int off = LANES / 2; off >= 1; off >>= 1)
+                mx = fmaxf(mx, __shfl_xor(mx, off, 64));
+            const float use = mx == -INFINITY ? 0.0f : mx, old = __builtin_amdgcn_exp2f((m - use) * c2);
+            const float f = lane < n ? __builtin_amdgcn_exp2f((st[0] - use) * c2) : 0.0f;
+            m = mx;
+            l = l * old + (lane < n ? st[1] * f : 0.0f);
+            v *= old;
+            for (uint32_t k0 = 0u;;) {
+#pragma unroll
+                for (uint32_t e = 0; e < AHEAD; ++e)
+                    v += x[e] * __shfl(f, (int)(min(k0 + e, LANES - 1u) + (threadIdx.x & 63u) / LANES * LANES), 64);
+                k0 += AHEAD;
+                if (k0 >= n)
+                    break;
+                load(k0);
+            }
+        }
+#pragma unroll
+        for (int off = LANES / 2; off >= 1; off >>= 1)
+            l += __shfl_xor(l, off, 64);
+        const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+        const uint32_t token = start + row / a.group, qh = h * a.group + row % a.group;
+        if (d < (uint32_t)D) {
+            const u32x2 two = {pack2<DT>(v[0] * inv, v[1] * inv), pack2<DT>(v[2] * inv, v[3] * inv)};
+            *reinterpret_cast<u32x2 *>(a.o + token * a.o_token + qh * a.o_head + d * 2u) = two;
+        }
+        if (a.lse && lane == 0u)
+            a.lse[(uint64_t)token * a.heads + qh] = l == 0.0f ? -INFINITY : (m * c2 - kLift<DT> + __log2f(l)) * kLn2;
     };
     single_tile_loop(g, n_tiles, prologue, body);
 }
@@ -1057,7 +1098,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttArgs a, SGDRC_SE
 
 typedef void (*AttKernel)(AttArgs, const uint32_t *, const uint32_t *, const int32_t *, const int32_t *, uint32_t, Gate);
 typedef void (*JoinKernel)(AttArgs, const uint32_t *, const uint32_t *, const int32_t *, const int32_t *, uint32_t,
-                           uint32_t, Gate);
+                           uint32_t, uint32_t, Gate);
 
 // How a call's rows are spread, by the most rows a segment can have: the
 // kernel, its wavefronts, blocks of 16 rows of each, and the ranges that the
@@ -1195,9 +1236,6 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     const uint64_t blocks_of_rows = (max_nodes * group + rb - 1u) / rb;
     if (seg * blocks_of_rows * cache->kv_heads > (1ull << 31) / blocks->n_requests)
         return set_error(SGDRC_EINVAL, "more than 2^31 steps of %u tokens at full tables", kStep);
-    const uint64_t join_tiles = ((uint64_t)n_tokens * n_heads + kJoinRows - 1u) / kJoinRows;
-    if (join_tiles >= (1ull << 31) - 65536u)
-        return set_error(SGDRC_EINVAL, "too many tokens");
     if (n_tokens && ((rc = check_rows(q, "q")) || (rc = check_rows(o, "o"))))
         return rc;
     Ctx *c = nullptr;
@@ -1239,10 +1277,13 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     SGDRC_HIP(hipGetLastError());
     if ((rc = finish_static_tlog(g, s)))
         return rc;
+    const uint32_t chunks = (std::min(max_nodes * group, rb) + join_rows(cache->head_dim) - 1u) /
+                            join_rows(cache->head_dim);
+    const uint32_t join_tiles = (f.ranges - 1u) * chunks;
     if ((rc = make_gate(c, stream, join_tiles, kStreamGroupCus, &g, &li, false, true)))
         return rc;
     hipLaunchKernelGGL(join, dim3(gated_grid(c, att_occupancy(join, kAttThreads), join_tiles, li)), dim3(kAttThreads), 0, s, a,
-                       d_q_start, blocks->table, d_lens, d_totals, rb, (uint32_t)join_tiles, g);
+                       d_q_start, blocks->table, d_lens, d_totals, rb, chunks, join_tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);
 }
