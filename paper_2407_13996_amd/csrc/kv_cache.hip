@@ -201,42 +201,44 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
     single_tile_loop(g, n_tiles, prologue, body);
 }
 
-constexpr int kAppendTokens = 16;  // tokens of an append tile
-// A tile's V rows: its tokens and those of an aligned group of 8 slots that
-// begins in it.
-constexpr int kAppendRows = kAppendTokens + 7;
-
-// A tile is 16 tokens of one head.  K goes to the cache as it comes, 16 bytes
+// A tile is TOKENS tokens of one head.  K goes to the cache as it comes, 16 bytes
 // at a time; V is turned, the 8 tokens of an aligned group of slots meeting
 // in one 16-byte store, through LDS.  Groups that the tokens do not fill are
 // written element by element (every token of a decoding step; the ends of a
-// prompt's run).  A group belongs to the tile of its first token.
-template <int D>
+// prompt's run).  A group belongs to the tile of its first token.  Bound by
+// the way from slots and rows through LDS to the stores, which a tile of 32
+// goes half as often: 16384 tokens of 8 heads take 32 us so (4.2 TB/s) and 36
+// in tiles of 16; 61 tokens, which do not fill the GPU either way, 6.3 and 5.1.
+template <int D, int TOKENS>
 __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, RowsView v,
                                                           const int64_t *__restrict__ slots,
                                                           uint32_t n_tokens, uint32_t n_tiles, Gate g)
 {
+    constexpr int kRows = TOKENS + 7;                     // the tile's and those of a group that begins in it
     constexpr uint32_t V16 = D / 8;                       // 16-byte pieces of a row
     constexpr uint32_t kBack = 7u;                        // tokens before the tile that are looked at
-    constexpr uint32_t kSeen = kBack + kAppendTokens + 7u;
+    constexpr uint32_t kSeen = kBack + TOKENS + 7u;
     __shared__ int64_t s_slot[kSeen];
     __shared__ uint32_t s_bits[2];                        // leaders of full groups, single tokens
-    __shared__ __attribute__((aligned(16))) uint16_t s_v[kAppendRows][D + 8];
-    constexpr uint32_t kLoads = (kAppendTokens * V16 + kKvThreads - 1u) / kKvThreads;
+    __shared__ uint32_t s_lead[TOKENS / 8 + 1];    // the leaders
+    __shared__ __attribute__((aligned(16))) uint16_t s_v[kRows][D + 8];
+    constexpr uint32_t kLoads = (TOKENS * V16 + kKvThreads - 1u) / kKvThreads;
     auto body = [&](uint32_t t, uint32_t &err) {
-        const uint32_t h = t % c.heads, t0 = t / c.heads * (uint32_t)kAppendTokens;
+        const uint32_t h = t % c.heads, t0 = t / c.heads * (uint32_t)TOKENS;
         // K's lanes: 16 tokens side by side (256-byte runs of the cache); V's
         // lanes: along the rows
+        const auto k_tok = [](uint32_t i) { return i / (16u * V16) * 16u + i % 16u; };
+        const auto k_d8 = [](uint32_t i) { return i % (16u * V16) / 16u; };
         u32x4 kk[kLoads], vv[kLoads];
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) {
             const uint32_t i = j * kKvThreads + threadIdx.x;
-            const uint32_t tk = min(t0 + i % kAppendTokens, n_tokens - 1u);
+            const uint32_t tk = min(t0 + k_tok(i), n_tokens - 1u);
             const uint32_t tv = min(t0 + i / V16, n_tokens - 1u);
             const u32x4 z = {0u, 0u, 0u, 0u};
             kk[j] = vv[j] = z;
-            if (i < kAppendTokens * V16) {
-                kk[j] = *reinterpret_cast<const u32x4 *>(k.ptr + tk * k.token + h * k.head + (i / kAppendTokens) * 16u);
+            if (i < TOKENS * V16) {
+                kk[j] = *reinterpret_cast<const u32x4 *>(k.ptr + tk * k.token + h * k.head + k_d8(i) * 16u);
                 vv[j] = *reinterpret_cast<const u32x4 *>(v.ptr + tv * v.token + h * v.head + (i % V16) * 16u);
             }
         }
@@ -254,7 +256,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
         if (threadIdx.x < 64u) {
             // token ``threadIdx.x`` of the tile: does it lead a full group, or stand alone
             bool lead = false, single = false;
-            if (threadIdx.x < (uint32_t)kAppendTokens) {
+            if (threadIdx.x < (uint32_t)TOKENS) {
                 const uint32_t x = threadIdx.x + kBack;
                 const int64_t s = s_slot[x];
                 if (s >= 0) {
@@ -268,6 +270,8 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
                 }
             }
             const uint64_t lb = __ballot(lead), sb = __ballot(single);
+            if (lead)
+                s_lead[__popcll(lb & ((1ull << threadIdx.x) - 1ull))] = threadIdx.x;
             if (threadIdx.x == 0u) {
                 s_bits[0] = (uint32_t)lb;
                 s_bits[1] = (uint32_t)sb;
@@ -276,12 +280,11 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) {
             const uint32_t i = j * kKvThreads + threadIdx.x;
-            if (i < kAppendTokens * V16) {
-                const int64_t s = s_slot[kBack + i % kAppendTokens];
+            if (i < TOKENS * V16) {
+                const int64_t s = s_slot[kBack + k_tok(i)];
                 if (s >= 0) {
                     uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
-                    *reinterpret_cast<u32x4 *>(at + k_off<D>(i / kAppendTokens, (uint32_t)s & ((1u << c.bshift) - 1u),
-                                                             c.bshift)) = kk[j];
+                    *reinterpret_cast<u32x4 *>(at + k_off<D>(k_d8(i), (uint32_t)s & ((1u << c.bshift) - 1u), c.bshift)) = kk[j];
                 }
                 *reinterpret_cast<u32x4 *>(&s_v[i / V16][(i % V16) * 8u]) = vv[j];
             }
@@ -290,30 +293,29 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
         const uint32_t leaders = __builtin_amdgcn_readfirstlane(s_bits[0]);
         const uint32_t singles = __builtin_amdgcn_readfirstlane(s_bits[1]);
         // the rows past the tile of its last group (tokens that exist: their slots are consecutive)
-        if (leaders >> (kAppendTokens - 7)) {
+        if (leaders >> (TOKENS - 7)) {
             const uint32_t last = 31u - (uint32_t)__builtin_clz(leaders);
-            const uint32_t n = (last + 8u - kAppendTokens) * V16;
+            const uint32_t n = (last + 8u - TOKENS) * V16;
             for (uint32_t i = threadIdx.x; i < n; i += kKvThreads)
-                *reinterpret_cast<u32x4 *>(&s_v[kAppendTokens + i / V16][(i % V16) * 8u]) =
-                    *reinterpret_cast<const u32x4 *>(v.ptr + (uint64_t)(t0 + kAppendTokens + i / V16) * v.token +
+                *reinterpret_cast<u32x4 *>(&s_v[TOKENS + i / V16][(i % V16) * 8u]) =
+                    *reinterpret_cast<const u32x4 *>(v.ptr + (uint64_t)(t0 + TOKENS + i / V16) * v.token +
                                                      h * v.head + (i % V16) * 16u);
             __syncthreads();
         }
-        for (uint32_t todo = leaders; todo; todo &= todo - 1u) {
-            const uint32_t x = (uint32_t)__builtin_ctz(todo);
+        // a thread takes 16 bytes of a group: a dimension of its eight tokens
+        for (uint32_t i = threadIdx.x; i < (uint32_t)__builtin_popcount(leaders) * D; i += kKvThreads) {
+            const uint32_t x = s_lead[i / (uint32_t)D], d = i % (uint32_t)D;
             const int64_t s = s_slot[kBack + x];
             uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
             const uint32_t t8 = ((uint32_t)s & ((1u << c.bshift) - 1u)) >> 3;
-            for (uint32_t d = threadIdx.x; d < (uint32_t)D; d += kKvThreads) {
-                u32x4 o;
+            u32x4 o;
 #pragma unroll
-                for (uint32_t q = 0; q < 4u; ++q)
-                    o[q] = (uint32_t)s_v[x + 2u * q][d] | ((uint32_t)s_v[x + 2u * q + 1u][d] << 16);
-                *reinterpret_cast<u32x4 *>(at + v_off<D>(t8, d, c.bshift)) = o;
-            }
+            for (uint32_t q = 0; q < 4u; ++q)
+                o[q] = (uint32_t)s_v[x + 2u * q][d] | ((uint32_t)s_v[x + 2u * q + 1u][d] << 16);
+            *reinterpret_cast<u32x4 *>(at + v_off<D>(t8, d, c.bshift)) = o;
         }
         if (singles) {
-            for (uint32_t i = threadIdx.x; i < (uint32_t)(kAppendTokens * D); i += kKvThreads) {
+            for (uint32_t i = threadIdx.x; i < (uint32_t)(TOKENS * D); i += kKvThreads) {
                 const uint32_t x = i / (uint32_t)D, d = i % (uint32_t)D;
                 if ((singles >> x) & 1u) {
                     const int64_t s = s_slot[kBack + x];
@@ -535,14 +537,26 @@ static int launch_tiles(sgdrc_ctx *ctx, void *stream, uint64_t tiles, int occ, K
     return finish_static_tlog(g, s);
 }
 
+// Tiles of 16 tokens as long as the GPU holds them all at once.
+constexpr uint64_t kAppendShort = 2048;
+
+template <int D, int TOKENS>
+static int launch_append_tiles(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer, const sgdrc_rows *k,
+                               const sgdrc_rows *v, const int64_t *slots, uint32_t n_tokens, void *stream)
+{
+    static const int occ = occupancy(k_kv_append<D, TOKENS>, kKvThreads);
+    const uint64_t tiles = ((uint64_t)n_tokens + TOKENS - 1u) / TOKENS * cache->kv_heads;
+    return launch_tiles(ctx, stream, tiles, occ, k_kv_append<D, TOKENS>, kv_view(cache, layer), rows_view(k),
+                        rows_view(v), slots, n_tokens);
+}
+
 template <int D>
 static int launch_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer, const sgdrc_rows *k,
                          const sgdrc_rows *v, const int64_t *slots, uint32_t n_tokens, void *stream)
 {
-    static const int occ = occupancy(k_kv_append<D>, kKvThreads);
-    const uint64_t tiles = ((uint64_t)n_tokens + kAppendTokens - 1u) / kAppendTokens * cache->kv_heads;
-    return launch_tiles(ctx, stream, tiles, occ, k_kv_append<D>, kv_view(cache, layer), rows_view(k), rows_view(v),
-                        slots, n_tokens);
+    return ((uint64_t)n_tokens + 15u) / 16u * cache->kv_heads <= kAppendShort
+               ? launch_append_tiles<D, 16>(ctx, cache, layer, k, v, slots, n_tokens, stream)
+               : launch_append_tiles<D, 32>(ctx, cache, layer, k, v, slots, n_tokens, stream);
 }
 
 template <int D>
@@ -602,7 +616,7 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
     int rc = check_kv_cache(cache);
     if (rc || (rc = kv_layer(cache, layer)))
         return rc;
-    if (n_tokens > 0x7FFFFFFFu || (uint64_t)n_tokens * cache->kv_heads / kAppendTokens >= (1ull << 31) - 65536u)
+    if (n_tokens > 0x7FFFFFFFu || (uint64_t)n_tokens * cache->kv_heads / 16u >= (1ull << 31) - 65536u)
         return set_error(SGDRC_EINVAL, "too many tokens");
     if (n_tokens && ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v")) ||
                      (rc = check_aligned(d_slots, 8, "slots"))))
