@@ -8,8 +8,7 @@
 namespace sgdrc {
 
 constexpr int kKvThreads = 256;
-constexpr uint32_t kMapRequests = 256;   // requests of a map tile
-constexpr uint32_t kMapTokens = 1024;    // tokens of a map tile
+constexpr uint32_t kMapTile = kKvThreads;  // requests and tokens of a map tile, one a thread
 constexpr uint32_t kRefused = 0xFFFFFFFFu;
 
 struct MapArgs {
@@ -52,7 +51,8 @@ __device__ __forceinline__ MapAsk map_ask(const MapArgs &a, uint32_t r)
 // between workgroups does: its requests' and tokens' entries follow from the
 // sums in LDS.  The state goes to other memory than it is read from for the
 // same reason.  A step is bound by the launch and this chain of round trips
-// (lengths, sums, table or ring, slot), not by its bytes.
+// (lengths, sums, table or ring, slot), not by its bytes: 8 requests take 4.8
+// us, 2048 of which 9 end 13.5 (17 in tiles of four tokens a thread).
 __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_tiles, Gate g)
 {
     __shared__ uint32_t s_q[SGDRC_MAX_REQUESTS + 1];  // first token of each request
@@ -103,6 +103,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
         for (int k = 0; k < 3; ++k)
             for (uint32_t w = 0; w < wave; ++w)
                 run[k] += s_sum[k][w];
+        uint32_t taken = 0u, given = 0u;  // ends of the last pages taken and given back
         for (uint32_t r = r0; r < r1; ++r) {
             const MapAsk q = map_ask(a, r);
             s_q[r] = (uint32_t)min(run[0], (uint64_t)a.n_tokens);
@@ -116,26 +117,30 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
             else
                 s_e[r] = served ? (uint32_t)(q.need ? run[1] : 0u) : kRefused;
             if (served && q.need)
-                atomicMax(&s_taken, (uint32_t)end);
+                taken = (uint32_t)end;
             if (fits && q.freed)
-                atomicMax(&s_given, (uint32_t)back);
+                given = (uint32_t)back;
             run[1] = end;
             run[2] = back;
             if (r == R - 1u)
                 s_q[R] = (uint32_t)min(run[0], (uint64_t)a.n_tokens);
         }
+        if (taken)
+            atomicMax(&s_taken, taken);
+        if (given)
+            atomicMax(&s_given, given);
     };
     auto body = [&](uint32_t t, uint32_t &err) {
         err |= pro_err;
         const uint32_t lane = threadIdx.x & 63u;
-        const uint32_t taken_at = (uint32_t)(taken0 % a.ring_size);
+        const uint32_t taken_at = (uint32_t)(taken0 % a.ring_size), put_at = (uint32_t)(put0 % a.ring_size);
         if (t == 0u && threadIdx.x == 0u) {
             a.ring_pos_out[0] = taken0 + s_taken;
             a.ring_pos_out[1] = put0 + s_given;
             a.q_start[R] = s_q[R];
         }
         {
-            const uint32_t r = t * kMapRequests + threadIdx.x;
+            const uint32_t r = t * kMapTile + threadIdx.x;
             uint32_t freed = 0u;
             if (r < R) {
                 const MapAsk q = map_ask(a, r);
@@ -148,20 +153,33 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
                 a.q_start[r] = s_q[r];
                 freed = on ? q.freed : 0u;
             }
-            // ended requests' pages, a wavefront for one request at a time
-            for (uint64_t todo = __ballot(freed != 0u); todo; todo &= todo - 1ull) {
-                const uint32_t l = (uint32_t)__builtin_ctzll(todo);
-                const uint32_t rr = t * kMapRequests + (threadIdx.x & ~63u) + l;
-                const uint32_t n = __shfl(freed, l, 64);
-                for (uint32_t b = lane; b < n; b += 64u)
-                    a.ring[(put0 + s_e[rr] + b) % a.ring_size] = a.table[(uint64_t)rr * a.stride + b];
+            // ended requests' pages, a wavefront for four requests at a time
+            for (uint64_t todo = __ballot(freed != 0u); todo;) {
+                uint32_t rr[4], n[4], most = 0u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t l = todo ? (uint32_t)__builtin_ctzll(todo) : 0u;
+                    rr[k] = t * kMapTile + (threadIdx.x & ~63u) + l;
+                    n[k] = todo ? __shfl(freed, l, 64) : 0u;
+                    most = max(most, n[k]);
+                    todo &= todo - 1ull;
+                }
+                for (uint32_t b = lane; b < most; b += 64u) {
+                    uint32_t page[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        page[k] = a.table[(uint64_t)rr[k] * a.stride + min(b, max(n[k], 1u) - 1u)];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (b < n[k]) {
+                            const uint64_t at = (uint64_t)put_at + s_e[rr[k]] + b;  // below twice the ring's size
+                            a.ring[at >= a.ring_size ? at - a.ring_size : at] = page[k];
+                        }
+                }
             }
         }
-#pragma unroll
-        for (uint32_t j = 0; j < kMapTokens / kKvThreads; ++j) {
-            const uint64_t i = (uint64_t)t * kMapTokens + j * kKvThreads + threadIdx.x;
-            if (i >= a.n_tokens)
-                continue;
+        const uint64_t i = (uint64_t)t * kMapTile + threadIdx.x;
+        if (i < a.n_tokens) {
             int64_t slot = -1;
             int32_t req = -1, pos = -1;
             if (i < s_q[R]) {
@@ -603,8 +621,8 @@ int colored_kv_map(sgdrc_ctx *ctx, uint32_t block_tokens, const sgdrc_kv_state *
     const MapArgs a = {in->ring_pos, in->held, in->lens, d_new, out->ring_pos, out->held, out->lens, d_ring,
                        blocks->table, d_q_start, d_slots, d_request, d_position, ring_size, blocks->stride,
                        (uint32_t)__builtin_ctz(block_tokens), blocks->n_requests, n_tokens};
-    const uint64_t tiles = std::max<uint64_t>((blocks->n_requests + kMapRequests - 1u) / kMapRequests,
-                                              ((uint64_t)n_tokens + kMapTokens - 1u) / kMapTokens);
+    const uint64_t tiles = std::max<uint64_t>((blocks->n_requests + kMapTile - 1u) / kMapTile,
+                                              ((uint64_t)n_tokens + kMapTile - 1u) / kMapTile);
     static const int occ = occupancy(k_kv_map, kKvThreads);
     return launch_tiles(ctx, stream, tiles, occ, k_kv_map, a);
 }
