@@ -52,7 +52,7 @@ __device__ __forceinline__ MapAsk map_ask(const MapArgs &a, uint32_t r)
 // sums in LDS.  The state goes to other memory than it is read from for the
 // same reason.  A step is bound by the launch and this chain of round trips
 // (lengths, sums, table or ring, slot), not by its bytes: 8 requests take 4.8
-// us, 2048 of which 9 end 13.5 (17 in tiles of four tokens a thread).
+// us, 2048 of which every ninth ends 13.5 (17 in tiles of four tokens a thread).
 __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_tiles, Gate g)
 {
     __shared__ uint32_t s_q[SGDRC_MAX_REQUESTS + 1];  // first token of each request
