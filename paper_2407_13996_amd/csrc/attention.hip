@@ -314,6 +314,15 @@ __device__ __forceinline__ float row_sum(float v)
     return q.a + q.b;
 }
 
+// ``v``, as a value that the compiler cannot know before this point: what
+// follows from it is worked out here, not kept in registers through the loops
+// above.
+__device__ __forceinline__ uint32_t fresh(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // n low bits, n of any size.
 __device__ __forceinline__ uint32_t low8(int32_t n)
 {
@@ -431,13 +440,22 @@ struct Rows {
     float m[NB], l[NB];
     uint32_t tok[NB], node[NB];
 
-    __device__ __forceinline__ void begin(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t col, uint32_t grp)
+    // block b's rows: 16 from row0 + apart * b on
+    __device__ __forceinline__ uint32_t find(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t apart, uint32_t col,
+                                             int b)
+    {
+        const uint32_t row = min(row0 + apart * b + col, x.rows - 1u);
+        node[b] = row / a.group;
+        tok[b] = x.start + node[b];
+        return row;
+    }
+
+    __device__ __forceinline__ void begin(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t apart, uint32_t col,
+                                          uint32_t grp)
     {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const uint32_t row = min(row0 + 16u * b + col, x.rows - 1u);
-            node[b] = row / a.group;
-            tok[b] = x.start + node[b];
+            const uint32_t row = find(a, x, row0, apart, col, b);
             const uint8_t *const qp = a.q.ptr + tok[b] * a.q.token + (x.h * a.group + row % a.group) * a.q.head;
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk)
@@ -453,12 +471,12 @@ struct Rows {
 
 // Scores capped to cap tanh(s scale / cap), in units of log 2; tanh y = 1 -
 // 2 / (1 + e^2y).
-template <int NB>
+template <int NB, int ACT = NB>
 __device__ __forceinline__ void cap_scores(const AttArgs &a, f32x4 (&s)[NB][2])
 {
     const float in = a.scale / a.softcap * 2.0f * kLog2e, out = a.softcap * kLog2e;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < ACT; ++b)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -475,12 +493,13 @@ constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
 
 // Scores to weights: the running maximum, what was summed under the old one
 // rescaled, the weights added up and rounded to the P^T operand.  A row's
-// sum stays spread over its four lanes until the end.
-template <int DT, int D, int NB>
+// sum stays spread over its four lanes until the end.  ACT: the blocks that
+// have rows, the first ones.
+template <int DT, int D, int NB, int ACT = NB>
 __device__ __forceinline__ void weigh(Rows<DT, D, NB> &w, const f32x4 (&s)[NB][2], float c2, u32x4 (&pf)[NB])
 {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int b = 0; b < ACT; ++b) {
         float mx = fmaxf(s[b][0][0], s[b][0][1]);
 #pragma unroll
         for (int i = 2; i < 8; ++i)
@@ -641,7 +660,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB 
             const Piece x = take_piece(a, sq, s_line, 16u * NB, t, lo, hi, p);
             p += x.u1 - x.u0;
             Rows<DT, D, NB> w;
-            w.begin(a, x, 0u, col, grp);
+            w.begin(a, x, 0u, 16u, col, grp);
             const uint32_t *const row_table = sq.table + (uint64_t)x.r * a.stride;
             const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
             const uint32_t bmask = (1u << a.c.bshift) - 1u;
@@ -804,7 +823,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     constexpr uint32_t T = 64u * NW;
     constexpr uint32_t kRows = 16u * NB * NW;
     constexpr int KK = D / 32, DD = D / 16;
-    constexpr int VH = DD / 2;                               // V's operands at a time
+    constexpr bool kTight = NB == 2 || D == 256;             // registers are short
+    constexpr int VH = kTight ? DD / 4 : DD / 2;             // V's operands at a time
     constexpr uint32_t kPieces = 8u * D;                     // of 16 bytes: K's, then V's
     constexpr uint32_t PER = (kPieces + T - 1u) / T;         // a thread's
     constexpr uint32_t kBuf = kPieces * 16u;
@@ -835,33 +855,38 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
             const Piece x = take_piece(a, sq, s_line, kRows, t, lo, hi, p);
             p += x.u1 - x.u0;
             Rows<DT, D, NB> w;
-            w.begin(a, x, x.row0 + 16u * NB * wave, col, grp);
+            w.begin(a, x, x.row0 + 16u * wave, 16u * NW, col, grp);
             const uint32_t *const row_table = sq.table + (uint64_t)x.r * a.stride;
             const uint8_t *const head = a.c.pool + x.h * head_bytes<D>(a.c.bshift);
             const int32_t drafted = (int32_t)(x.total - x.ctx);
             u32x4 st[2][PER];
             uint32_t bads[2] = {0u, 0u};
-            auto fetch = [&](uint32_t u, const StepPages &sp, u32x4 (&to)[PER], uint32_t &bad) __attribute__((always_inline)) {
+            auto fetch = [&](uint32_t tid, uint32_t u, const StepPages &sp, u32x4 (&to)[PER], uint32_t &bad) __attribute__((always_inline)) {
                 const StepAt at = step_at(a, head, sp, x.total, err);
                 bad = at.bad;
                 const uint32_t off = u * kStep & bmask;
 #pragma unroll
                 for (uint32_t j = 0; j < PER; ++j) {
-                    const uint32_t i = j * T + threadIdx.x;
+                    const uint32_t i = j * T + tid;
                     if (kPieces % T == 0u || i < kPieces)
                         to[j] = *reinterpret_cast<const u32x4 *>(
                             (half_of(i) ? at.p[1] : at.p[0]) + place_of(i) + off * (i < kPieces / 2u ? 16u : 2u * D));
                 }
             };
-            // ``edge``: a step that some row does not see whole
-            auto step = [&](auto edge, uint32_t u, u32x4 (&from)[PER], uint32_t &bad_of, uint8_t *buf,
+            // ``edge``: a step that some row does not see whole; ``active``: this
+            // wavefront's blocks that have rows
+                auto step = [&](auto edge, auto active, uint32_t tid, uint32_t u, u32x4 (&from)[PER], uint32_t &bad_of, uint8_t *buf,
                             StepPages &ahead) __attribute__((always_inline)) {
+                constexpr int ACT = active;
+                // worked out every time where registers are short: spilled, waiting
+                // for its reload would wait for the data on its way too
+                const uint32_t in_step = kTight ? fresh(tid) : tid, col = in_step & 15u, grp = in_step >> 4 & 3u;
                 const uint32_t bad = bad_of;
                 uint32_t odd = 0u;
                 if constexpr (edge) {
 #pragma unroll
                     for (uint32_t j = 0; j < PER; ++j) {
-                        const uint32_t i = j * T + threadIdx.x;
+                        const uint32_t i = j * T + tid;
                         if (i >= kPieces / 2u && i < kPieces) {
                             const uint32_t t8 = (i - kPieces / 2u) / D;
                             const int32_t j0 = (int32_t)(u * kStep + t8 * 8u) - (int32_t)x.ctx;
@@ -871,7 +896,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                 }
 #pragma unroll
                 for (uint32_t j = 0; j < PER; ++j) {
-                    const uint32_t i = j * T + threadIdx.x;
+                    const uint32_t i = j * T + tid;
                     if (kPieces % T == 0u || i < kPieces)
                         *reinterpret_cast<u32x4 *>(buf + i * 16u) = from[j];
                 }
@@ -882,8 +907,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                 // past the piece's end its last step again: where loads may or may
                 // not have been made, the compiler has to wait for all of them
                 // before it uses older ones
-                fetch(min(u + 2u, x.u1 - 1u), ahead, from, bad_of);
+                fetch(tid, min(u + 2u, x.u1 - 1u), ahead, from, bad_of);
                 ahead = step_pages(row_table, x, min(u + 3u, x.u1 - 1u), a.c.bshift);
+                if constexpr (ACT == 0)
+                    return;
                 const uint8_t *const kb = buf + (grp * 32u + col) * 16u;
                 const uint8_t *const vb = buf + kBuf / 2u + (grp * D + col) * 16u;
                 // operands in groups, each requested while the one before is
@@ -898,12 +925,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
+                    for (int b = 0; b < ACT; ++b)
                         s[b][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk) {
 #pragma unroll
-                        for (int b = 0; b < NB; ++b)
+                        for (int b = 0; b < ACT; ++b)
                             s[b][q] = att_mfma<DT>(kf[kk], w.q[b][kk], s[b][q]);
                         if (q == 0)
                             kf[kk] = *reinterpret_cast<const u32x4 *>(kb + kk * 2048 + 256);
@@ -915,7 +942,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                     vf[dd] = *reinterpret_cast<const u32x4 *>(vb + dd * 256);
                 __builtin_amdgcn_sched_barrier(0);
                 if (a.softcap > 0.0f)
-                    cap_scores<NB>(a, s);
+                    cap_scores<NB, ACT>(a, s);
                 u32x4 pf[NB];
                 uint32_t seen[NB];
                 if constexpr (edge) {
@@ -923,7 +950,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                     const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
                     mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
                 }
-                weigh<DT, D, NB>(w, s, c2, pf);
+                weigh<DT, D, NB, ACT>(w, s, c2, pf);
                 if (edge && odd != 0u) {
                     add_odd<DT, D, NB>(w, pf, seen, [&](int dd) {
                         return *reinterpret_cast<const u32x4 *>(vb + dd * 256);
@@ -932,15 +959,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
                     for (int dd = 0; dd < DD; ++dd) {
 #pragma unroll
-                        for (int b = 0; b < NB; ++b)
+                        for (int b = 0; b < ACT; ++b)
                             w.acc[b][dd] = att_mfma<DT>(vf[dd % VH], pf[b], w.acc[b][dd]);
                         if (dd + VH < DD)
                             vf[dd % VH] = *reinterpret_cast<const u32x4 *>(vb + (dd + VH) * 256);
                     }
                 }
             };
-            fetch(x.u0, step_pages(row_table, x, x.u0, a.c.bshift), st[0], bads[0]);
-            fetch(min(x.u0 + 1u, x.u1 - 1u), step_pages(row_table, x, min(x.u0 + 1u, x.u1 - 1u), a.c.bshift), st[1],
+            fetch(threadIdx.x, x.u0, step_pages(row_table, x, x.u0, a.c.bshift), st[0], bads[0]);
+            fetch(threadIdx.x, min(x.u0 + 1u, x.u1 - 1u), step_pages(row_table, x, min(x.u0 + 1u, x.u1 - 1u), a.c.bshift), st[1],
                   bads[1]);
             StepPages ahead = step_pages(row_table, x, min(x.u0 + 2u, x.u1 - 1u), a.c.bshift);
             // steps that every row sees whole in a loop of their own, two at a
@@ -948,22 +975,38 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
             // accumulators every time
             const uint32_t seen_steps = min(x.u1, x.ctx / kStep);
             uint32_t u = x.u0;
-            for (; u + 2u <= seen_steps && (bads[0] | bads[1]) == 0u; u += 2u) {
-                step(std::false_type(), u, st[0], bads[0], s_kv, ahead);
-                step(std::false_type(), u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
-            }
+            auto whole = [&](auto active) __attribute__((always_inline)) {
+                for (; u + 2u <= seen_steps && (bads[0] | bads[1]) == 0u; u += 2u) {
+                    step(std::false_type(), active, threadIdx.x, u, st[0], bads[0], s_kv, ahead);
+                    step(std::false_type(), active, threadIdx.x, u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
+                }
+            };
+            // (all wavefronts meet the same barriers, whichever loop they are in)
+            const uint32_t first = x.row0 + 16u * wave;
+            if (NB == 2 && first + 16u * NW < x.rows)
+                whole(std::integral_constant<int, NB>());
+            else if (first < x.rows)
+                whole(std::integral_constant<int, 1>());
+            else
+                whole(std::integral_constant<int, 0>());
+            const uint32_t edge_tid = fresh(threadIdx.x);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                w.find(a, x, first, 16u * NW, edge_tid & 15u, b);
             for (; u < x.u1; u += 2u) {
-                step(std::true_type(), u, st[0], bads[0], s_kv, ahead);
+                step(std::true_type(), std::integral_constant<int, NB>(), edge_tid, u, st[0], bads[0], s_kv, ahead);
                 if (u + 1u < x.u1)
-                    step(std::true_type(), u + 1u, st[1], bads[1], s_kv + kBuf, ahead);
+                    step(std::true_type(), std::integral_constant<int, NB>(), edge_tid, u + 1u, st[1], bads[1], s_kv + kBuf,
+                         ahead);
             }
+            const uint32_t end_tid = fresh(threadIdx.x), col_e = end_tid & 15u, grp_e = end_tid >> 4 & 3u;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const uint32_t in = 16u * (NB * wave + b) + col;
-                const float f = put_stats<DT, D>(a, x, kRows, in, w.m[b], row_sum(w.l[b]), c2, grp == 0u);
+                const uint32_t in = 16u * (NW * b + wave) + col_e;
+                const float f = put_stats<DT, D>(a, x, kRows, in, w.m[b], row_sum(w.l[b]), c2, grp_e == 0u);
 #pragma unroll
                 for (int dd = 0; dd < DD; ++dd)
-                    put_row<DT, D>(a, x, kRows, in, dd * 16u + grp * 4u, w.acc[b][dd] * f);
+                    put_row<DT, D>(a, x, kRows, in, dd * 16u + grp_e * 4u, w.acc[b][dd] * f);
             }
             __syncthreads();  // the last step is read
         }
