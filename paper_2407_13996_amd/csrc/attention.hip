@@ -450,8 +450,8 @@ struct Rows {
         return row;
     }
 
-    __device__ __forceinline__ void begin(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t apart, uint32_t col,
-                                          uint32_t grp)
+    __device__ __forceinline__ void load_q(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t apart, uint32_t col,
+                                           uint32_t grp)
     {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -460,6 +460,15 @@ struct Rows {
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk)
                 q[b][kk] = *reinterpret_cast<const u32x4 *>(qp + (kk * 4u + grp) * 16u);
+        }
+    }
+
+    __device__ __forceinline__ void begin(const AttArgs &a, const Piece &x, uint32_t row0, uint32_t apart, uint32_t col,
+                                          uint32_t grp)
+    {
+        load_q(a, x, row0, apart, col, grp);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
             m[b] = -INFINITY;
             l[b] = 0.0f;
 #pragma unroll
@@ -990,9 +999,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
             else
                 whole(std::integral_constant<int, 0>());
             const uint32_t edge_tid = fresh(threadIdx.x);
+            // Q is read again where registers are short: kept over both loops,
+            // some of it was spilled in the first
+            if constexpr (kTight) {
+                asm volatile("" ::: "memory");
+                w.load_q(a, x, first, 16u * NW, edge_tid & 15u, edge_tid >> 4 & 3u);
+            } else {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                w.find(a, x, first, 16u * NW, edge_tid & 15u, b);
+                for (int b = 0; b < NB; ++b)
+                    w.find(a, x, first, 16u * NW, edge_tid & 15u, b);
+            }
             for (; u < x.u1; u += 2u) {
                 step(std::true_type(), std::integral_constant<int, NB>(), edge_tid, u, st[0], bads[0], s_kv, ahead);
                 if (u + 1u < x.u1)
