@@ -15,7 +15,7 @@
 //
 // Split: every request's tokens are cut in steps of 32, and the steps of all
 // (request, block of rows, head) triples, "segments", form one line, which is
-// cut in kRanges equal ranges, one tile of the schedule each, whatever the
+// cut in at most 512 equal ranges, one tile of the schedule each, whatever the
 // lengths: long and short requests fill the device alike.  A range's piece of a
 // segment that is not all of it leaves its maximum, sum and weighted V in
 // the workspace; a second launch joins them.  The cut depends on the lengths
@@ -638,18 +638,22 @@ __device__ __forceinline__ float put_stats(const AttArgs &a, const Piece &x, uin
     return !x.whole ? 1.0f : l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // NaN stays NaN
 }
 
-// Few rows (16 NB of a segment at most): bound by the cache's bytes.  The four
+// Few rows (16 of a segment at most): bound by the cache's bytes.  The four
 // wavefronts share the rows and take every fourth step.  K and V go from
-// memory to the MFMA operands' registers; the next step's K is requested as
-// soon as the scores have taken this one's, the next V after the products with
-// this one, into the same registers, so that a wavefront has a step in flight
-// for the registers of one.
-template <int DT, int D, int NB>
-__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(NB == 1 && D < 256 ? 2 : 1))) void k_attend_few(AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
+// memory to the MFMA operands' registers, past the L2, which nothing would
+// read them from again; the next step's K is requested as soon as the scores
+// have taken this one's, the next V after the products with this one, into the
+// same registers, so that a wavefront has a step in flight for the registers
+// of one.  96 requests of up to 24000 tokens (4.7 GB, 32 query and 8 key heads
+// of 128) take 710 us, 6.7 TB/s; one of 1009 tokens 7, of which launch, plan
+// and the first loads are nearly all.
+template <int DT, int D>
+__global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D < 256 ? 2 : 1))) void k_attend_few(
+    AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
 {
     const Seqs sq = {q_start, table, lens, totals};
     constexpr uint32_t WK = kAttWaves;
-    constexpr int KK = D / 32, DD = D / 16;
+    constexpr int NB = 1, KK = D / 32, DD = D / 16;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
     __shared__ float s_ml[kAttWaves][16 * NB][2];
@@ -824,7 +828,17 @@ __device__ __forceinline__ uint32_t lds_token(uint32_t p)
 // V pass through LDS once for all of them.  Every thread moves its share of a
 // step, 16 bytes at a time, in the order of memory, which is the order of the
 // MFMA operands: two steps ahead into registers, then to one of two LDS
-// buffers, so that one barrier a step is enough.
+// buffers, so that one barrier a step is enough.  Blocks of 16 rows go to the
+// wavefronts in turn, and a wavefront leaves out those that a segment does not
+// have: 192 rows are three blocks on every SIMD.
+//
+// Bound by the step's chain: the barrier, the operands from LDS (16 KiB a
+// wavefront and step at head_dim 128), products, softmax, products follow each
+// other, in both wavefronts of a SIMD at the same time, and their times add up
+// (measured for 64 requests of 192 rows over up to 8192 tokens, 8 key heads:
+// 370 us, where the arithmetic takes 210 at the rate of a large plain product).  Wavefronts of 16 rows, four on a
+// SIMD, took 440, steps of 64 tokens 580, two groups of wavefronts half a step
+// apart 500 and more, each with registers spilled.
 template <int DT, int D, int NB, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void k_attend_many(AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
 {
@@ -1161,7 +1175,11 @@ typedef void (*JoinKernel)(AttArgs, const uint32_t *, const uint32_t *, const in
 
 // How a call's rows are spread, by the most rows a segment can have: the
 // kernel, its wavefronts, blocks of 16 rows of each, and the ranges that the
-// line of steps is cut in (as many as workgroups fit on 256 CUs).
+// line of steps is cut in (as many as workgroups fit on 256 CUs).  Both sides of
+// each limit, for 32 requests of 500 to 8000 tokens, 8 key heads of 128: 16 rows
+// 112 us in the form for few, 128 in one for 32 of the same kind; 32 rows 133
+// there, 130 here; 64 rows 139, in the form of 128 rows 151; 128 rows 189, in
+// the form of 256 273.  Heads of 256 leave no registers for two blocks.
 struct AttForm {
     bool many;
     uint32_t nb, waves, ranges;
@@ -1173,8 +1191,6 @@ static AttForm att_form(uint32_t dim, uint32_t rows)
 {
     if (rows <= 16u)
         return {false, 1, 4, dim == 256u ? 256u : 512u};
-    if (rows <= 32u && dim != 256u)
-        return {false, 2, 4, 256};
     if (rows <= 64u)
         return {true, 1, 4, 512};
     if (dim == 256u || rows <= 128u)
@@ -1185,12 +1201,8 @@ static AttForm att_form(uint32_t dim, uint32_t rows)
 template <int DT, int D>
 static AttKernel att_kernel_d(AttForm f)
 {
-    if (!f.many) {
-        if constexpr (D != 256)
-            if (f.nb == 2)
-                return k_attend_few<DT, D, 2>;
-        return k_attend_few<DT, D, 1>;
-    }
+    if (!f.many)
+        return k_attend_few<DT, D>;
     if (f.waves == 4)
         return k_attend_many<DT, D, 1, 4>;
     if constexpr (D != 256)
