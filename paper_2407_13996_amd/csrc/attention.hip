@@ -835,8 +835,9 @@ __device__ __forceinline__ uint32_t lds_token(uint32_t p)
 // Bound by the step's chain: the barrier, the operands from LDS (16 KiB a
 // wavefront and step at head_dim 128), products, softmax, products follow each
 // other, in both wavefronts of a SIMD at the same time, and their times add up
-// (measured for 64 requests of 192 rows over up to 8192 tokens, 8 key heads:
-// 370 us, where the arithmetic takes 210 at the rate of a large plain product).  Wavefronts of 16 rows, four on a
+// (measured for 24 requests of 64 nodes, 64 query and 8 key heads, over 2000 to
+// 8000 tokens: 370 us, where the arithmetic takes 210 at the rate of a large
+// plain product).  Wavefronts of 16 rows, four on a
 // SIMD, took 440, steps of 64 tokens 580, two groups of wavefronts half a step
 // apart 500 and more, each with registers spilled.
 template <int DT, int D, int NB, int NW>
@@ -1059,7 +1060,7 @@ constexpr uint32_t kMostRanges = 512;
 // were written whole.  Every workgroup first lists those segments, a cut
 // between ranges a thread, the first cut of a segment having it; a tile is
 // some rows of one of them.  (Tiles by rows of the output, each with its
-// request and cuts to find, took 88 us for 64 requests of 24 nodes and 17 for
+// request and cuts to find, took 88 us for 24 requests of 512 rows and 17 for
 // one long cache, where these take 25 and 11.)
 // Bound by latency: a row's pieces are asked for eight at a time.
 template <int DT, int D>
