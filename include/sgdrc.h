@@ -530,11 +530,14 @@ typedef struct {
     uint32_t dtype;
 } sgdrc_kv_cache;
 
-/* Block tables: row r of ``stride`` entries is request r's (device). */
+/* Block tables (device): request r's row is the ``width`` entries from
+ * table + r * stride on.  What lies between the rows of a table that is part
+ * of a wider one (width < stride) is neither read nor written. */
 typedef struct {
     uint32_t *table;
-    uint32_t stride;
+    uint32_t stride;       /* entries from a row to the next */
     uint32_t n_requests;   /* 1..4096 */
+    uint32_t width;        /* entries of a row, at most stride; 0: stride of them */
 } sgdrc_kv_blocks;
 
 /* Rows of heads: element d of head h of token t is at
@@ -576,8 +579,8 @@ typedef struct {
  * ring_size: at least the pages in circulation.  n_tokens: entries of
  * d_slots, d_request and d_position (0 is valid, with those NULL).  EINVAL: NULL or misaligned
  * pointers, in and out sharing a pointer, block_tokens not a power of two in
- * 16..1024, n_requests outside 1..4096, stride * block_tokens above 2^31 - 1,
- * ring_size 0, n_tokens above 2^31 - 1. */
+ * 16..1024, n_requests outside 1..4096, stride 0, width above stride,
+ * width * block_tokens above 2^31 - 1, ring_size 0, n_tokens above 2^31 - 1. */
 int colored_kv_map(sgdrc_ctx *ctx, uint32_t block_tokens, const sgdrc_kv_state *in,
                    const sgdrc_kv_state *out, uint32_t *d_ring, uint32_t ring_size,
                    const sgdrc_kv_blocks *blocks, const int32_t *d_new, uint32_t *d_q_start,

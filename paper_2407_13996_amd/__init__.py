@@ -81,7 +81,8 @@ class KvCache(ctypes.Structure):
 
 
 class KvBlocks(ctypes.Structure):
-    _fields_ = [("table", ctypes.c_void_p), ("stride", ctypes.c_uint32), ("n_requests", ctypes.c_uint32)]
+    _fields_ = [("table", ctypes.c_void_p), ("stride", ctypes.c_uint32), ("n_requests", ctypes.c_uint32),
+                ("width", ctypes.c_uint32)]
 
 
 class Rows(ctypes.Structure):
@@ -505,8 +506,11 @@ def _ints_of(t, name: str, size: int = 4):
 def _blocks(table) -> KvBlocks:
     if table.dim() != 2 or table.element_size() != 4 or table.is_floating_point() or table.stride(1) != 1:
         raise ValueError("table must be [requests, blocks] of 32-bit whole numbers, rows without gaps inside")
-    n = table.shape[0]
-    return KvBlocks(table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], n)
+    n, width = table.shape
+    if width == 0:
+        raise ValueError("the table's rows have no blocks")
+    # rows may lie apart, as in a slice of a wider table
+    return KvBlocks(table.data_ptr(), table.stride(0) if n > 1 else width, n, width)
 
 
 def _rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:

@@ -50,7 +50,7 @@ struct AttArgs {
     float *lse;
     const uint64_t *mask;
     float *work;
-    uint32_t n_requests, stride, n_tokens, max_nodes, mask_words;
+    uint32_t n_requests, stride, width, n_tokens, max_nodes, mask_words;
     uint32_t heads, group;      // query heads, query heads of a key/value head
     uint32_t most_ranges;       // pieces that the line of steps is cut in at most
     float scale, softcap;
@@ -81,7 +81,7 @@ __device__ __forceinline__ Req load_req(const AttArgs &a, const Seqs &sq, uint32
     Req q;
     const uint32_t s = sq.q_start[r], e = sq.q_start[r + 1u];
     const int32_t total = sq.totals[r], ctx = sq.lens[r];
-    const uint32_t cap = a.stride << a.c.bshift;
+    const uint32_t cap = a.width << a.c.bshift;
     q.start = min(s, a.n_tokens);
     const uint32_t end = max(min(e, a.n_tokens), q.start);
     q.nodes = min(end - q.start, a.max_nodes);
@@ -1304,7 +1304,7 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     const uint32_t group = n_heads / cache->kv_heads;
     const AttForm f = att_form(cache->head_dim, max_nodes * group);
     const uint32_t rb = f.rows();
-    const uint64_t seg = ((uint64_t)blocks->stride * cache->block_tokens + kStep - 1u) / kStep;
+    const uint64_t seg = ((uint64_t)blocks_width(blocks) * cache->block_tokens + kStep - 1u) / kStep;
     const uint64_t blocks_of_rows = (max_nodes * group + rb - 1u) / rb;
     if (seg * blocks_of_rows * cache->kv_heads > (1ull << 31) / blocks->n_requests)
         return set_error(SGDRC_EINVAL, "more than 2^31 steps of %u tokens at full tables", kStep);
@@ -1327,6 +1327,7 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
     a.work = static_cast<float *>(d_work);
     a.n_requests = blocks->n_requests;
     a.stride = blocks->stride;
+    a.width = blocks_width(blocks);
     a.n_tokens = n_tokens;
     a.max_nodes = max_nodes;
     a.mask_words = mask_words;

@@ -21,7 +21,7 @@ struct MapArgs {
     uint32_t *q_start;
     int64_t *slots;
     int32_t *request, *position;
-    uint32_t ring_size, stride, bshift, n_requests, n_tokens;
+    uint32_t ring_size, stride, width, bshift, n_requests, n_tokens;
 };
 
 // What a request asks for.  ``ok``: its state is sound and its tokens fit its
@@ -37,9 +37,9 @@ __device__ __forceinline__ MapAsk map_ask(const MapArgs &a, uint32_t r)
     MapAsk q;
     q.ended = fresh < 0;
     q.tokens = q.ended ? 0u : (uint32_t)fresh;
-    q.ok = len >= 0 && held >= 0 && held <= (int64_t)a.stride && len <= (held << a.bshift);
+    q.ok = len >= 0 && held >= 0 && held <= (int64_t)a.width && len <= (held << a.bshift);
     const int64_t total = len + (int64_t)q.tokens;
-    q.ok = q.ok && total <= ((int64_t)a.stride << a.bshift);
+    q.ok = q.ok && total <= ((int64_t)a.width << a.bshift);
     const int64_t blocks = (total + (1 << a.bshift) - 1) >> a.bshift;
     q.need = q.ok && !q.ended && blocks > held ? (uint32_t)(blocks - held) : 0u;
     q.freed = q.ok && q.ended ? (uint32_t)held : 0u;
@@ -352,7 +352,7 @@ struct CommitArgs {
     const uint32_t *table;
     const int32_t *lens, *path, *accepted;
     int32_t *lens_out;
-    uint32_t stride, path_stride;
+    uint32_t stride, width, path_stride;
 };
 
 constexpr uint32_t kCommitBatch = 8;  // path entries whose loads are in flight together
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a
     auto body = [&](uint32_t t, uint32_t &err) {
         const uint32_t r = t % n_requests, layer = t / n_requests;
         const int32_t len = a.lens[r], want = a.accepted[r];
-        const int32_t cap = (int32_t)(a.stride << c.bshift);
+        const int32_t cap = (int32_t)(a.width << c.bshift);
         const bool sound = len >= 0 && len <= cap && want >= 0;
         const uint32_t n = sound ? min((uint32_t)want, a.path_stride) : 0u;
         __syncthreads();  // the last tile's LDS is read
@@ -515,8 +515,11 @@ int check_kv_blocks(const sgdrc_kv_blocks *b, uint32_t block_tokens)
         return set_error(SGDRC_EINVAL, "blocks is NULL");
     if (b->n_requests < 1 || b->n_requests > SGDRC_MAX_REQUESTS)
         return set_error(SGDRC_EINVAL, "n_requests %u outside 1..%d", b->n_requests, SGDRC_MAX_REQUESTS);
-    if (b->stride < 1 || (uint64_t)b->stride * block_tokens > 0x7FFFFFFFull)
-        return set_error(SGDRC_EINVAL, "a table row of %u blocks: none, or 2^31 tokens or more", b->stride);
+    const uint32_t width = blocks_width(b);
+    if (width < 1 || (uint64_t)width * block_tokens > 0x7FFFFFFFull)
+        return set_error(SGDRC_EINVAL, "a table row of %u blocks: none, or 2^31 tokens or more", width);
+    if (width > b->stride)
+        return set_error(SGDRC_EINVAL, "a table row of %u blocks, %u entries apart", width, b->stride);
     return check_aligned(b->table, 4, "blocks.table");
 }
 
@@ -625,7 +628,7 @@ int colored_kv_map(sgdrc_ctx *ctx, uint32_t block_tokens, const sgdrc_kv_state *
         return rc;
     const MapArgs a = {in->ring_pos, in->held, in->lens, d_new, out->ring_pos, out->held, out->lens, d_ring,
                        blocks->table, d_q_start, d_slots, d_request, d_position, ring_size, blocks->stride,
-                       (uint32_t)__builtin_ctz(block_tokens), blocks->n_requests, n_tokens};
+                       blocks_width(blocks), (uint32_t)__builtin_ctz(block_tokens), blocks->n_requests, n_tokens};
     const uint64_t tiles = std::max<uint64_t>((blocks->n_requests + kMapTile - 1u) / kMapTile,
                                               ((uint64_t)n_tokens + kMapTile - 1u) / kMapTile);
     static const int occ = occupancy(k_kv_map, kKvThreads);
@@ -672,7 +675,7 @@ int colored_kv_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_k
     if (path_stride < 1 || path_stride > SGDRC_MAX_NODES)
         return set_error(SGDRC_EINVAL, "path_stride %u outside 1..%d", path_stride, SGDRC_MAX_NODES);
     const CommitArgs a = {cache->n_layers > 1 ? cache->layer_stride : 0, blocks->table, d_lens, d_path, d_accepted,
-                          d_lens_out, blocks->stride, path_stride};
+                          d_lens_out, blocks->stride, blocks_width(blocks), path_stride};
     switch (cache->head_dim) {
     case 64: return launch_commit<64>(ctx, cache, a, blocks->n_requests, stream);
     case 96: return launch_commit<96>(ctx, cache, a, blocks->n_requests, stream);

@@ -54,6 +54,9 @@ inline KvView kv_view(const sgdrc_kv_cache *c, uint32_t layer)
             (uint32_t)__builtin_ctz(c->block_tokens), c->kv_heads};
 }
 
+// Entries of a row of block tables.
+inline uint32_t blocks_width(const sgdrc_kv_blocks *b) { return b->width ? b->width : b->stride; }
+
 inline RowsView rows_view(const sgdrc_rows *r)
 {
     return {static_cast<const uint8_t *>(r->ptr), r->token_stride * 2u, r->head_stride * 2u};
