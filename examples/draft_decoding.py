@@ -125,7 +125,7 @@ class Server:
             words += [[(r >> 64 * k) & (1 << 64) - 1 for k in range(MOST // 64)] for r in rows]
         mask = torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in words], dtype=torch.int64,
                             device=DEV)
-        totals, q_start, slots = self.map(counts, n)
+        self.totals, q_start, slots = self.map(counts, n)
         at = self.lens.repeat_interleave(torch.tensor(counts, device=DEV)).long() + torch.tensor(depth, device=DEV)
         x = self.w.embed[tokens].float() + self.w.place[at].float()
         for layer in range(LAYERS):
@@ -133,7 +133,7 @@ class Server:
             q, k, v = qkv[:, :HEADS], qkv[:, HEADS:HEADS + KV], qkv[:, HEADS + KV:]
             sg.colored_kv_append(self.ctx, self.cache, layer, k, v, slots)
             o = torch.empty(n, HEADS, DIM, dtype=torch.bfloat16, device=DEV)
-            sg.colored_tree_attention(self.ctx, self.cache, layer, q, q_start, self.table, self.lens, totals, o,
+            sg.colored_tree_attention(self.ctx, self.cache, layer, q, q_start, self.table, self.lens, self.totals, o,
                                       self.work, mask=mask, max_nodes=MOST, scale=DIM ** -0.5)
             x = x + self.w.apply(self.ctx, f"out{layer}", o.view(n, HEADS * DIM))
         best = self.w.apply(self.ctx, "logits", norm(x)).argmax(1).tolist()
@@ -146,7 +146,8 @@ class Server:
             path[r, :len(p)] = torch.tensor(p, dtype=torch.int32)
         accepted = torch.tensor([len(p) for p in paths], dtype=torch.int32, device=DEV)
         lens = torch.empty_like(self.lens)
-        sg.colored_kv_commit(self.ctx, self.cache, self.table, self.lens, path.to(DEV), accepted, lens)
+        sg.colored_kv_commit(self.ctx, self.cache, self.table, self.lens, path.to(DEV), accepted, lens,
+                             totals=self.totals)
         self.lens = lens
 
     def end(self):

@@ -45,7 +45,7 @@
  *    threads; operations on one stream are ordered, operations on different
  *    streams may run concurrently (each stream gets its own work queue).
  *  - The cache calls (colored_kv_map, colored_kv_append, colored_kv_commit,
- *    colored_tree_attention) enqueue kernels only and may be captured too.
+ *    colored_kv_commit_within, colored_tree_attention) enqueue kernels only and may be captured too.
  *    What the host cannot know -- lengths, slots, block tables -- they read
  *    on the device and check there: what is out of range is skipped and
  *    raises SGDRC_DEVERR_SEQ (pages: SGDRC_DEVERR_PT_RANGE).
@@ -503,8 +503,8 @@ int colored_gemv_form(uint32_t allowed_cus, uint32_t schedule, int w_dtype, uint
  * A step of decoding with drafts: colored_kv_map gives every request the
  * pages for its new tokens and every token its slot; for each layer,
  * colored_kv_append writes K and V and colored_tree_attention reads them;
- * once the accepted path of each draft is known, colored_kv_commit closes it
- * up in all layers.  Lengths and states are double-buffered: each call reads
+ * once the accepted path of each draft is known, colored_kv_commit_within closes
+ * it up in all layers.  Lengths and states are double-buffered: each call reads
  * one set and writes another. */
 #define SGDRC_MAX_REQUESTS 4096
 #define SGDRC_MAX_NODES 256
@@ -602,11 +602,25 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
  * d_lens_out[r] = d_lens[r] + d_accepted[r] (d_lens_out must not be d_lens).
  * Tokens past the path keep what they hold.  A path that does not ascend, is
  * longer than path_stride or leaves the table's row is cut there, and raises
+ * SGDRC_DEVERR_SEQ.  A token of the path whose page the pool does not have is
+ * not moved and raises SGDRC_DEVERR_PT_RANGE; it counts in d_lens_out, and
+ * colored_tree_attention skips it likewise.
+ * Every token of the path must be the request's own: d_accepted[r] must be 0
+ * for a request that colored_kv_map did not serve (its row's entries past its
+ * blocks may name other requests' pages).  colored_kv_commit_within sees to that by
+ * d_totals, the tokens in each request's cache with its draft (the lengths
+ * that colored_kv_map wrote): the path is cut at the first token past them too,
+ * so that a request that was not served keeps its length, and a total
+ * below d_lens[r] or past the table's row accepts nothing; both raise
  * SGDRC_DEVERR_SEQ.  EINVAL: a bad cache, NULL or misaligned pointers,
  * path_stride outside 1..256, as colored_kv_map for the blocks. */
 int colored_kv_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks,
                       const int32_t *d_lens, const int32_t *d_path, uint32_t path_stride,
                       const int32_t *d_accepted, int32_t *d_lens_out, void *stream);
+int colored_kv_commit_within(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks,
+                             const int32_t *d_lens, const int32_t *d_totals, const int32_t *d_path,
+                             uint32_t path_stride, const int32_t *d_accepted, int32_t *d_lens_out,
+                             void *stream);
 
 /* Attention of each request's new tokens, the nodes of a tree of drafted
  * tokens, over its cache.  Request r's nodes are the tokens

@@ -152,6 +152,7 @@ def lib() -> ctypes.CDLL:
                                i32),
             "colored_kv_append": ([vp, P(KvCache), u32, P(Rows), P(Rows), vp, u32, vp], i32),
             "colored_kv_commit": ([vp, P(KvCache), P(KvBlocks), vp, vp, u32, vp, vp, vp], i32),
+            "colored_kv_commit_within": ([vp, P(KvCache), P(KvBlocks), vp, vp, vp, u32, vp, vp, vp], i32),
             "colored_tree_attention": ([vp, P(KvCache), u32, P(Rows), u32, vp, u32, u32, P(KvBlocks), vp, vp, vp, u32,
                                         ctypes.c_float, ctypes.c_float, P(Rows), vp, vp, u64, vp], i32),
             "sgdrc_tree_attention_workspace": ([P(KvCache), u32, u32, P(u64)], i32),
@@ -560,16 +561,25 @@ def colored_kv_append(ctx, cache: KvCache, layer: int, k, v, slots, stream=None)
                                    _ints_of(slots, "slots", 8), n, _stream(stream)))
 
 
-def colored_kv_commit(ctx, cache: KvCache, table, lens, path, accepted, lens_out, stream=None) -> None:
+def colored_kv_commit(ctx, cache: KvCache, table, lens, path, accepted, lens_out, stream=None, totals=None) -> None:
     """Closes up each request's accepted path (``path`` [requests, most], the
-    first ``accepted`` entries of a row) in all layers; lens_out = lens + accepted."""
+    first ``accepted`` entries of a row) in all layers; lens_out = lens + accepted.
+    ``totals``: the lengths that colored_kv_map wrote; a path is cut where it leaves
+    them, so that a request that was not served keeps its length.  Without them
+    ``accepted`` must be 0 for such a request."""
     blocks = _blocks(table)
     n = blocks.n_requests
     if not (lens.numel() == accepted.numel() == lens_out.numel() == n and path.dim() == 2 and path.shape[0] == n):
         raise ValueError("the arrays' lengths do not fit the table's requests")
-    _check(lib().colored_kv_commit(_h(ctx), cache, blocks, _ints_of(lens, "lens"), _ints_of(path, "path"),
-                                   path.shape[1], _ints_of(accepted, "accepted"), _ints_of(lens_out, "lens_out"),
-                                   _stream(stream)))
+    if totals is not None and totals.numel() != n:
+        raise ValueError("the arrays' lengths do not fit the table's requests")
+    rest = (_ints_of(path, "path"), path.shape[1], _ints_of(accepted, "accepted"), _ints_of(lens_out, "lens_out"),
+            _stream(stream))
+    if totals is None:
+        _check(lib().colored_kv_commit(_h(ctx), cache, blocks, _ints_of(lens, "lens"), *rest))
+    else:
+        _check(lib().colored_kv_commit_within(_h(ctx), cache, blocks, _ints_of(lens, "lens"),
+                                              _ints_of(totals, "totals"), *rest))
 
 
 def tree_attention_workspace(cache: KvCache, n_heads: int, max_nodes: int) -> int:

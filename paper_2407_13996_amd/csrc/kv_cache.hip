@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
 struct CommitArgs {
     uint64_t layer_stride;
     const uint32_t *table;
-    const int32_t *lens, *path, *accepted;
+    const int32_t *lens, *totals, *path, *accepted;  // totals: may be NULL
     int32_t *lens_out;
     uint32_t stride, width, path_stride;
 };
@@ -378,7 +378,8 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a
         const uint32_t r = t % n_requests, layer = t / n_requests;
         const int32_t len = a.lens[r], want = a.accepted[r];
         const int32_t cap = (int32_t)(a.width << c.bshift);
-        const bool sound = len >= 0 && len <= cap && want >= 0;
+        const int32_t total = a.totals ? a.totals[r] : cap;
+        const bool sound = len >= 0 && len <= total && total <= cap && want >= 0;
         const uint32_t n = sound ? min((uint32_t)want, a.path_stride) : 0u;
         __syncthreads();  // the last tile's LDS is read
         if (threadIdx.x == 0u)
@@ -390,7 +391,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a
         if (i < n) {
             node = a.path[(uint64_t)r * a.path_stride + i];
             const int32_t prev = i ? a.path[(uint64_t)r * a.path_stride + i - 1u] : -1;
-            if (node <= prev || node >= cap - len)
+            if (node <= prev || node >= total - len)
                 atomicMin(&s_n, i);
         }
         __syncthreads();
@@ -594,6 +595,30 @@ static int launch_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const Comm
                         n_requests);
 }
 
+static int commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks, const int32_t *d_lens,
+                  const int32_t *d_totals, const int32_t *d_path, uint32_t path_stride, const int32_t *d_accepted,
+                  int32_t *d_lens_out, void *stream)
+{
+    int rc = check_kv_cache(cache);
+    if (rc || (rc = check_kv_blocks(blocks, cache->block_tokens)))
+        return rc;
+    if ((rc = check_aligned(d_lens, 4, "lens")) || (rc = check_aligned(d_path, 4, "path")) ||
+        (rc = check_aligned(d_accepted, 4, "accepted")) || (rc = check_aligned(d_lens_out, 4, "lens_out")))
+        return rc;
+    if (d_lens == d_lens_out || d_totals == d_lens_out)
+        return set_error(SGDRC_EINVAL, "lens_out shares memory with lens or totals");
+    if (path_stride < 1 || path_stride > SGDRC_MAX_NODES)
+        return set_error(SGDRC_EINVAL, "path_stride %u outside 1..%d", path_stride, SGDRC_MAX_NODES);
+    const CommitArgs a = {cache->n_layers > 1 ? cache->layer_stride : 0, blocks->table, d_lens, d_totals, d_path, d_accepted,
+                          d_lens_out, blocks->stride, blocks_width(blocks), path_stride};
+    switch (cache->head_dim) {
+    case 64: return launch_commit<64>(ctx, cache, a, blocks->n_requests, stream);
+    case 96: return launch_commit<96>(ctx, cache, a, blocks->n_requests, stream);
+    case 128: return launch_commit<128>(ctx, cache, a, blocks->n_requests, stream);
+    default: return launch_commit<256>(ctx, cache, a, blocks->n_requests, stream);
+    }
+}
+
 }  // namespace sgdrc
 
 using namespace sgdrc;
@@ -664,24 +689,17 @@ int colored_kv_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_k
                       int32_t *d_lens_out, void *stream)
 {
     clear_error();
-    int rc = check_kv_cache(cache);
-    if (rc || (rc = check_kv_blocks(blocks, cache->block_tokens)))
-        return rc;
-    if ((rc = check_aligned(d_lens, 4, "lens")) || (rc = check_aligned(d_path, 4, "path")) ||
-        (rc = check_aligned(d_accepted, 4, "accepted")) || (rc = check_aligned(d_lens_out, 4, "lens_out")))
-        return rc;
-    if (d_lens == d_lens_out)
-        return set_error(SGDRC_EINVAL, "lens and lens_out share memory");
-    if (path_stride < 1 || path_stride > SGDRC_MAX_NODES)
-        return set_error(SGDRC_EINVAL, "path_stride %u outside 1..%d", path_stride, SGDRC_MAX_NODES);
-    const CommitArgs a = {cache->n_layers > 1 ? cache->layer_stride : 0, blocks->table, d_lens, d_path, d_accepted,
-                          d_lens_out, blocks->stride, blocks_width(blocks), path_stride};
-    switch (cache->head_dim) {
-    case 64: return launch_commit<64>(ctx, cache, a, blocks->n_requests, stream);
-    case 96: return launch_commit<96>(ctx, cache, a, blocks->n_requests, stream);
-    case 128: return launch_commit<128>(ctx, cache, a, blocks->n_requests, stream);
-    default: return launch_commit<256>(ctx, cache, a, blocks->n_requests, stream);
-    }
+    return commit(ctx, cache, blocks, d_lens, nullptr, d_path, path_stride, d_accepted, d_lens_out, stream);
+}
+
+int colored_kv_commit_within(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks,
+                             const int32_t *d_lens, const int32_t *d_totals, const int32_t *d_path,
+                             uint32_t path_stride, const int32_t *d_accepted, int32_t *d_lens_out, void *stream)
+{
+    clear_error();
+    const int rc = check_aligned(d_totals, 4, "totals");
+    return rc ? rc
+              : commit(ctx, cache, blocks, d_lens, d_totals, d_path, path_stride, d_accepted, d_lens_out, stream);
 }
 
 }  // extern "C"
