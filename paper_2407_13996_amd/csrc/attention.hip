@@ -1198,11 +1198,16 @@ typedef void (*JoinKernel)(AttArgs, const uint32_t *, const uint32_t *, const in
 
 // How a call's rows are spread, by the most rows a segment can have: the
 // kernel, its wavefronts, blocks of 16 rows of each, and the ranges that the
-// line of steps is cut in (as many as workgroups fit on 256 CUs).  Both sides of
-// each limit, for 32 requests of 500 to 8000 tokens, 8 key heads of 128: 16 rows
-// 112 us in the form for few, 128 in one for 32 of the same kind; 32 rows 133
-// there, 130 here; 64 rows 139, in the form of 128 rows 151; 128 rows 189, in
-// the form of 256 273.  Heads of 256 leave no registers for two blocks.
+// line of steps is cut in: 512 where two workgroups fit a CU, 256 where one
+// does, so that all are at work at once.  Both sides of each limit, for 32
+// requests of 500 to 8000 tokens, 8 key heads of 128: 16 rows 112 us in the
+// form for few, 128 in one for 32 of the same kind; 32 rows 133 there, 130
+// here; 64 rows 139, in the form of 128 rows 151; 128 rows 189, in the form of
+// 256 273.  Heads of 256 leave no registers for two blocks, and no LDS for a
+// second workgroup: in 256 ranges 12 requests of up to 6000 tokens and 64 rows
+// take 129 us and one of 60000 and 32 rows 102, in 512 140 and 118 (two rounds,
+// twice the pieces to join); 32 requests of 500 to 8000 tokens, of 64 rows, 288
+// against 279, as shorter ranges end more evenly.
 struct AttForm {
     bool many;
     uint32_t nb, waves, ranges;
@@ -1215,7 +1220,7 @@ static AttForm att_form(uint32_t dim, uint32_t rows)
     if (rows <= 16u)
         return {false, 1, 4, dim == 256u ? 256u : 512u};
     if (rows <= 64u)
-        return {true, 1, 4, 512};
+        return {true, 1, 4, dim == 256u ? 256u : 512u};
     if (dim == 256u || rows <= 128u)
         return {true, 1, 8, 256};
     return {true, 2, 8, 256};
