@@ -636,11 +636,13 @@ int colored_kv_commit_within(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const 
  * sees, rounded to the cache's dtype, and d_lse (nullable; [n_tokens][n_heads]
  * fp32) receives log sum_j exp(s_ij).  A node that sees nothing gets zeros and
  * -infinity.  What a token that a node does not see holds, NaN and infinity
- * too, does not reach that node.  Scores, maxima and sums are fp32; exp(s)
- * is rounded to the cache's dtype where it is multiplied by V.  The order of
- * all sums depends on the lengths and shapes only, never on the CU mask:
- * results are bitwise reproducible.  Rows of tokens outside every request
- * are not written.
+ * too, does not reach that node.  Scores, maxima and sums are fp32.
+ * Where exp(s) is multiplied by V it is held in two numbers of the cache's dtype
+ * (16 bits in bf16, 22 in f16) if max_nodes * n_heads / kv_heads is 16 or less,
+ * and rounded to one if it is more, which adds as much to the error of o as
+ * its own rounding does.  The order of all sums depends on the lengths and
+ * shapes only, never on the CU mask: results are bitwise reproducible.  Rows of
+ * tokens outside every request are not written.
  * d_work: work_bytes of device memory, 256-byte aligned, at least
  * sgdrc_tree_attention_workspace's; used by the call until it is done, holds
  * nothing between calls.  max_nodes: no request has more nodes (those beyond

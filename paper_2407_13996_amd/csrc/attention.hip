@@ -522,12 +522,39 @@ __device__ __forceinline__ void cap_scores(const AttArgs &args, f32x4 (&s)[NB][2
 template <int DT>
 constexpr float kLift = DT == SGDRC_F16 ? 10.0f : 0.0f;
 
+// Two weights in two numbers each: a smaller one of the type, and what is left,
+// rounded.  Neither part of a weight is 0 (down to 2^-33 of the largest in f16),
+// so that an infinite value meets no 0.
+template <int DT>
+__device__ __forceinline__ void split2(float x, float y, uint32_t &most, uint32_t &rest)
+{
+    if (DT == SGDRC_BF16) {
+        // half a unit less, cut to 8 bits
+        const uint32_t bx = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, x), 0x8000u);
+        const uint32_t by = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, y), 0x8000u);
+        most = (bx >> 16) | (by & 0xFFFF0000u);
+        rest = pack2<DT>(x - __builtin_bit_cast(float, bx & 0xFFFF0000u), y - __builtin_bit_cast(float, by & 0xFFFF0000u));
+    } else {
+        constexpr float k = 1.0f - 0x1p-12f;
+        const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x * k, y * k));
+        most = __builtin_bit_cast(uint32_t, h);
+        rest = pack2<DT>(x - (float)h[0], y - (float)h[1]);
+    }
+}
+
 // Scores to weights: the running maximum, what was summed under the old one
-// rescaled, the weights added up and rounded to the P^T operand.  A row's
-// sum stays spread over its four lanes until the end.  ACT: the blocks that
-// have rows, the first ones.
-template <int DT, int D, int NB, int ACT = NB>
-__device__ __forceinline__ void weigh(Rows<DT, D, NB> &w, const f32x4 (&s)[NB][2], float c2, u32x4 (&pf)[NB])
+// rescaled, the weights added up (fp32) and brought to the P^T operand's type.
+// A row's sum stays spread over its four lanes until the end.  ACT: the blocks
+// that have rows, the first ones.  PARTS: the numbers of the type that hold a
+// weight, a product with V each.  With one, rounded to 8 bits in bf16 or 11 in
+// f16, the rounded weights add as much to the result's error as its own
+// rounding (24 nodes over 131001 tokens, bf16: 2.3e-3 of it off, 1.7e-3 of that by the
+// latter).  With two (16 bits and 22) nothing is added: the form for few rows waits
+// for memory and has the time (725 us either way for 96 requests of up to 24000
+// tokens).  The form for many has not: 495 us for 405 (24 requests of 64 nodes, 64 heads
+// on 8) and 151 for 130.
+template <int DT, int D, int NB, int PARTS, int ACT = NB>
+__device__ __forceinline__ void weigh(Rows<DT, D, NB> &w, const f32x4 (&s)[NB][2], float c2, u32x4 (&pf)[PARTS][NB])
 {
 #pragma unroll
     for (int b = 0; b < ACT; ++b) {
@@ -553,8 +580,16 @@ __device__ __forceinline__ void weigh(Rows<DT, D, NB> &w, const f32x4 (&s)[NB][2
             w.l[b] += p[i];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            pf[b][i] = pack2<DT>(p[2 * i], p[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (PARTS == 2) {
+                uint32_t most, rest;
+                split2<DT>(p[2 * i], p[2 * i + 1], most, rest);
+                pf[0][b][i] = most;
+                pf[1][b][i] = rest;
+            } else {
+                pf[0][b][i] = pack2<DT>(p[2 * i], p[2 * i + 1]);
+            }
+        }
     }
 }
 
@@ -577,8 +612,8 @@ __device__ __forceinline__ void mask_scores(const AttArgs &a, const Rows<DT, D, 
 // meet the weight 0 of a row that does not see them.  They are taken out of V,
 // and a product of marks counts those that each row sees: such a sum is
 // infinite or NaN, whatever the rest is.  ``load_v(dd)``: V^T's operand.
-template <int DT, int D, int NB, typename LoadV>
-__device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[NB], const uint32_t (&seen)[NB],
+template <int DT, int D, int NB, int PARTS, typename LoadV>
+__device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[PARTS][NB], const uint32_t (&seen)[NB],
                                         LoadV load_v)
 {
 #pragma unroll
@@ -586,7 +621,7 @@ __device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[NB
         u32x4 some, none;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const uint32_t sees = pair_mask(seen[b], w), weight = spread_top(top_from<1u>(pf[b][w]));
+            const uint32_t sees = pair_mask(seen[b], w), weight = spread_top(top_from<1u>(pf[0][b][w]) | top_from<1u>(pf[PARTS - 1][b][w]));
             some[w] = sees & weight & kOne<DT>;
             none[w] = sees & ~weight & kOne<DT>;
         }
@@ -600,7 +635,9 @@ __device__ __forceinline__ void add_odd(Rows<DT, D, NB> &r, const u32x4 (&pf)[NB
                 v[w] = two;
             }
             const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-            r.acc[b][dd] = att_mfma<DT>(v, pf[b], r.acc[b][dd]);
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k)
+                r.acc[b][dd] = att_mfma<DT>(v, pf[k][b], r.acc[b][dd]);
             const f32x4 n = att_mfma<DT>(marks, some, z), n0 = att_mfma<DT>(marks, none, z);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -675,7 +712,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D <
 {
     const Seqs sq = {q_start, table, lens, totals};
     constexpr uint32_t WK = kAttWaves;
-    constexpr int NB = 1, KK = D / 32, DD = D / 16;
+    constexpr int NB = 1, PARTS = 2, KK = D / 32, DD = D / 16;
     __shared__ uint32_t s_line[SGDRC_MAX_REQUESTS + 1];
     __shared__ uint32_t s_sum[kAttWaves];
     __shared__ float s_ml[kAttWaves][16 * NB][2];
@@ -749,12 +786,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D <
                     load_v(min(u + WK, x.u1 - 1u), at);
                     asm volatile("" ::: "memory");
                 };
-                auto products = [&](const u32x4 (&pf)[NB]) __attribute__((always_inline)) {
+                auto products = [&](const u32x4 (&pf)[PARTS][NB]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int dd = 0; dd < DD; ++dd)
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[b], w.acc[b][dd]);
+#pragma unroll
+                            for (int k = 0; k < PARTS; ++k)
+                                w.acc[b][dd] = att_mfma<DT>(vf[dd], pf[k][b], w.acc[b][dd]);
                 };
                 // steps that every row sees whole, in a loop of their own: with
                 // the others' code in it the compiler copies the accumulators
@@ -762,18 +801,18 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D <
                 const uint32_t seen_steps = min(x.u1, x.ctx / kStep);
                 for (; u < seen_steps && at.bad == 0u; u += WK) {
                     f32x4 s[NB][2];
-                    u32x4 pf[NB];
+                    u32x4 pf[PARTS][NB];
                     scores(s);
                     next_k();
                     if (a.softcap > 0.0f)
                         cap_scores<false, NB>(a, s);
-                    weigh<DT, D, NB>(w, s, c2, pf);
+                    weigh<DT, D, NB, PARTS>(w, s, c2, pf);
                     products(pf);
                     next_v();
                 }
                 for (; u < x.u1; u += WK) {
                     f32x4 s[NB][2];
-                    u32x4 pf[NB];
+                    u32x4 pf[PARTS][NB];
                     uint32_t seen[NB];
                     scores(s);
                     const uint32_t bad = at.bad;
@@ -787,9 +826,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D <
                     for (int dd = 0; dd < DD; ++dd)
                         odd |= keep_there<DT>(vf[dd], there);
                     mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
-                    weigh<DT, D, NB>(w, s, c2, pf);
+                    weigh<DT, D, NB, PARTS>(w, s, c2, pf);
                     if (__ballot(odd != 0u) != 0ull)
-                        add_odd<DT, D, NB>(w, pf, seen, [&](int dd) { return vf[dd]; });
+                        add_odd<DT, D, NB, PARTS>(w, pf, seen, [&](int dd) { return vf[dd]; });
                     else
                         products(pf);
                     next_v();
@@ -989,16 +1028,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                 for (int dd = 0; dd < VH; ++dd)
                     vf[dd] = *reinterpret_cast<const u32x4 *>(vb + dd * 256);
                 __builtin_amdgcn_sched_barrier(0);
-                u32x4 pf[NB];
+                u32x4 pf[1][NB];
                 uint32_t seen[NB];
                 if constexpr (edge) {
                     const int32_t j0 = (int32_t)(u * kStep + grp * 8u) - (int32_t)x.ctx;
                     const uint32_t there = (bad >> (grp >> 1)) & 1u ? 0u : low8(drafted - j0);
                     mask_scores<DT, D, NB>(a, w, j0, drafted, there, s, seen);
                 }
-                weigh<DT, D, NB, ACT>(w, s, c2, pf);
+                weigh<DT, D, NB, 1, ACT>(w, s, c2, pf);
                 if (edge && odd != 0u) {
-                    add_odd<DT, D, NB>(w, pf, seen, [&](int dd) {
+                    add_odd<DT, D, NB, 1>(w, pf, seen, [&](int dd) {
                         return *reinterpret_cast<const u32x4 *>(vb + dd * 256);
                     });
                 } else {
@@ -1006,7 +1045,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
                     for (int dd = 0; dd < DD; ++dd) {
 #pragma unroll
                         for (int b = 0; b < ACT; ++b)
-                            w.acc[b][dd] = att_mfma<DT>(vf[dd % VH], pf[b], w.acc[b][dd]);
+                            w.acc[b][dd] = att_mfma<DT>(vf[dd % VH], pf[0][b], w.acc[b][dd]);
                         if (dd + VH < DD)
                             vf[dd % VH] = *reinterpret_cast<const u32x4 *>(vb + (dd + VH) * 256);
                     }
