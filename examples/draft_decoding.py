@@ -12,7 +12,9 @@ page table names become the ring of free pages of the cache.  Every step
 * walks down each tree as far as the model's own choices go, and closes the
   accepted path up in the cache (colored_kv_commit).
 
-A prompt is a chain whose nodes are all accepted.  Run on an MI355X:
+A prompt is a chain whose nodes are all accepted.  A request for which the ring has
+too few pages accepts nothing and tries again in the next step; one that has
+its tokens ends, and its pages go to the others.  Run on an MI355X:
 
     python examples/draft_decoding.py
 """
@@ -86,10 +88,10 @@ def norm(x):
 class Server:
     """The requests' state: the cache, its block tables and the free pages."""
 
-    def __init__(self, ctx, weights, requests, most_tokens):
+    def __init__(self, ctx, weights, requests, most_tokens, blocks=None):
         self.ctx, self.w, self.n = ctx, weights, requests
         width = -(-most_tokens // BLOCK)
-        self.pool, free, pages = coloured_pages(ctx, requests * width)
+        self.pool, free, pages = coloured_pages(ctx, requests * width if blocks is None else blocks)
         self.ring = free.clone()      # all pages are free: the ring is the page table
         self.cache = sg.kv_cache(self.pool, pages, SHIFT, BLOCK, KV, DIM, sg.BF16, LAYERS, (1 << SHIFT) // LAYERS)
         self.ring_pos = torch.tensor([0, self.ring.numel()], dtype=torch.int64, device=DEV)
@@ -112,7 +114,10 @@ class Server:
 
     def step(self, trees):
         """The model's next token after every node of every request's tree;
-        trees[r]: (tokens, parents), a parent before its children, -1 the root's."""
+        trees[r]: (tokens, parents), a parent before its children, -1 the root's;
+        None: the request ends.  None for a request that found no pages."""
+        new = [-1 if t is None else len(t[0]) for t in trees]
+        trees = [t or ([], []) for t in trees]
         counts = [len(t) for t, _ in trees]
         n = sum(counts)
         tokens = torch.tensor([t for tree, _ in trees for t in tree], device=DEV)
@@ -125,7 +130,8 @@ class Server:
             words += [[(r >> 64 * k) & (1 << 64) - 1 for k in range(MOST // 64)] for r in rows]
         mask = torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in words], dtype=torch.int64,
                             device=DEV)
-        self.totals, q_start, slots = self.map(counts, n)
+        self.totals, q_start, slots = self.map(new, n)
+        self.lens = torch.where(torch.tensor(new, device=DEV) < 0, 0, self.lens)   # ended
         at = self.lens.repeat_interleave(torch.tensor(counts, device=DEV)).long() + torch.tensor(depth, device=DEV)
         x = self.w.embed[tokens].float() + self.w.place[at].float()
         for layer in range(LAYERS):
@@ -137,11 +143,12 @@ class Server:
                                       self.work, mask=mask, max_nodes=MOST, scale=DIM ** -0.5)
             x = x + self.w.apply(self.ctx, f"out{layer}", o.view(n, HEADS * DIM))
         best = self.w.apply(self.ctx, "logits", norm(x)).argmax(1).tolist()
-        return [best[sum(counts[:r]):sum(counts[:r + 1])] for r in range(self.n)]
+        grown = (self.totals - self.lens).tolist()
+        return [best[sum(counts[:r]):sum(counts[:r + 1])] if grown[r] == counts[r] else None for r in range(self.n)]
 
     def commit(self, paths):
         """Keeps the nodes paths[r] of the step's trees, in their order."""
-        path = torch.zeros(self.n, max(map(len, paths)), dtype=torch.int32)
+        path = torch.zeros(self.n, max(1, max(map(len, paths))), dtype=torch.int32)
         for r, p in enumerate(paths):
             path[r, :len(p)] = torch.tensor(p, dtype=torch.int32)
         accepted = torch.tensor([len(p) for p in paths], dtype=torch.int32, device=DEV)
@@ -187,26 +194,45 @@ def walk(tree, best):
         path.append(child[0])
 
 
-def decode(ctx, weights, prompts, n_new, depth):
-    """n_new tokens or a few more after each prompt, and the steps they took."""
-    server = Server(ctx, weights, len(prompts), max(map(len, prompts)) + n_new + 2 * depth + 2 + BLOCK)
+def decode(ctx, weights, prompts, n_new, depth, blocks=None, counts=None):
+    """n_new tokens or a few more after each prompt, and the steps they took, with
+    ``blocks`` pages for all requests (None: as many as they can need).
+    ``counts``: a dict that receives how many drafted nodes were accepted,
+    tokens moved in the cache and requests not served, over all steps."""
+    server = Server(ctx, weights, len(prompts), max(map(len, prompts)) + n_new + 2 * depth + 2 + BLOCK, blocks)
     seqs = [list(p) for p in prompts]
     trees = [(p, list(range(-1, len(p) - 1))) for p in prompts]   # chains
-    steps = 0
+    steps, ended, seen = 0, 0, {"accepted": 0, "moved": 0, "not served": 0}
     while True:
         best = server.step(trees)
-        walks = [walk(t, b) if steps else (list(range(len(t[0]))), b[-1:]) for t, b in zip(trees, best)]
-        server.commit([p for p, _ in walks])
-        for s, (_, more) in zip(seqs, walks):
+        paths = []
+        for s, p, t, b in zip(seqs, prompts, trees, best):
+            path, more = [], []
+            if t is None or b is None:
+                seen["not served"] += t is not None
+            elif len(s) == len(p):
+                path, more = list(range(len(p))), b[-1:]
+            else:
+                path, more = walk(t, b)
+                seen["accepted"] += len(path) - 1
+                seen["moved"] += sum(i != j for i, j in enumerate(path))
+            paths.append(path)
             s += more
+        server.commit(paths)
         steps += 1
-        # a request that has its tokens goes on without drafts until all have
+        if not any(paths) and trees.count(None) == ended:   # no page will become free
+            raise RuntimeError("too few pages for any request to go on")
+        ended = trees.count(None)
         if min(len(s) - len(p) for s, p in zip(seqs, prompts)) >= n_new:
             break
-        trees = [draft(s, depth if len(s) - len(p) < n_new else 0) for s, p in zip(seqs, prompts)]
+        # where the draft found no pages, the last token alone is next
+        trees = [None if len(s) - len(p) >= n_new else (p, list(range(-1, len(p) - 1))) if len(s) == len(p) else
+                 draft(s, 0 if b is None else depth) for s, p, b in zip(seqs, prompts, best)]
     free = server.end()
     assert free == server.ring.numel(), "a page was lost"
     assert ctx.device_error() == 0
+    if counts is not None:
+        counts.update(seen)
     return [s[len(p):len(p) + n_new] for s, p in zip(seqs, prompts)], steps
 
 
