@@ -220,7 +220,9 @@ def decode(ctx, weights, prompts, n_new, depth, blocks=None, counts=None):
             s += more
         server.commit(paths)
         steps += 1
-        if not any(paths) and trees.count(None) == ended:   # no page will become free
+        # no page becomes free, and no smaller draft is left to try
+        if not any(paths) and trees.count(None) == ended and all(
+                t is None or len(t[0]) == 1 or len(s) == len(p) for t, s, p in zip(trees, seqs, prompts)):
             raise RuntimeError("too few pages for any request to go on")
         ended = trees.count(None)
         if min(len(s) - len(p) for s, p in zip(seqs, prompts)) >= n_new:

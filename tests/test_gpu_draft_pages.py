@@ -72,3 +72,15 @@ def test_too_few_pages_for_anything(model):
         with pytest.raises(RuntimeError):
             dd.decode(ctx, weights, prompts_of(lengths, 1), N_NEW, 0, blocks=2 if len(lengths) == 1 else 6)
     ctx.device_error()
+
+
+def test_a_draft_that_does_not_fit_gives_way_to_its_root(model, monkeypatch):
+    """One request whose drafts of 40 nodes never find the pages that its tokens do."""
+    dd, ctx, weights = model
+    prompts = prompts_of((20,), 2)
+    monkeypatch.setattr(dd, "draft", lambda seq, depth: (seq[-1:] + [1] * 39 * (depth > 0),
+                                                         list(range(-1, 39 if depth else 0))))
+    counts = {}
+    new, _ = dd.decode(ctx, weights, prompts, N_NEW, 6, blocks=5, counts=counts)
+    check(dd, weights, prompts, new)
+    assert counts["not served"] > 0
