@@ -520,7 +520,20 @@ def _rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
         raise ValueError(f"{name} must be [tokens, {heads}, {dim}], the last dimension contiguous")
     if (F32, BF16, F16)[dtype] != _dtype_of(t):
         raise ValueError(f"{name} is not of the cache's dtype")
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    # a stride that no second token or head uses says nothing
+    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if heads > 1 else 0)
+
+
+def _written_rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
+    """The same for rows that are written: none of them may share memory."""
+    r = _rows(t, name, heads, dim, dtype)
+    spans = sorted((s, n) for s, n in ((t.stride(0), t.shape[0]), (t.stride(1), heads)) if n > 1)
+    end = dim
+    for stride, n in spans:
+        if stride < end:
+            raise ValueError(f"{name} has rows that overlap")
+        end += stride * (n - 1)
+    return r
 
 
 def _dtype_of(t) -> int:
@@ -606,6 +619,8 @@ def colored_tree_attention(ctx, cache: KvCache, layer: int, q, q_start, table, l
         if mask.dim() != 2 or mask.shape[0] != tokens:
             raise ValueError("mask must be [tokens, words]")
         words = mask.shape[1]
+    if not (hasattr(work, "data_ptr") and work.is_contiguous()):
+        raise ValueError("work must be a contiguous tensor")
     if lse is not None and not (_dtype_of(lse) == F32 and lse.is_contiguous() and lse.numel() == tokens * heads):
         raise ValueError("lse must be a contiguous fp32 tensor [tokens, heads]")
     _check(lib().colored_tree_attention(_h(ctx), cache, int(layer),
@@ -613,7 +628,7 @@ def colored_tree_attention(ctx, cache: KvCache, layer: int, q, q_start, table, l
                                         _ints_of(q_start, "q_start"), tokens, int(max_nodes), blocks,
                                         _ints_of(lens, "lens"), _ints_of(totals, "totals"),
                                         _ints_of(mask, "mask", 8), words, scale, softcap,
-                                        _rows(out, "out", heads, cache.head_dim, cache.dtype), _addr(lse),
+                                        _written_rows(out, "out", heads, cache.head_dim, cache.dtype), _addr(lse),
                                         _addr(work), work.numel() * work.element_size(), _stream(stream)))
 
 
