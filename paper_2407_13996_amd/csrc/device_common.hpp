@@ -23,7 +23,6 @@ constexpr uint32_t kDevErrPtRange = 1u;
 constexpr uint32_t kDevFlagGateFallback = 2u;
 constexpr uint32_t kDevErrSuspendedDropped = 4u;  // a suspended launch was discarded unresumed
 constexpr uint32_t kDevErrHandBack = 8u;          // a handed-back tile index out of range
-constexpr uint32_t kDevErrSeq = 16u;              // a length, row start, slot or path out of range
 
 // Queue slot states (QueueSlot::state).
 constexpr uint32_t kSlotIdle = 0u;
@@ -705,100 +704,6 @@ __device__ __forceinline__ void tile_loop(const Gate &g, uint32_t n_tiles, Prolo
         static_tile_loop(g, n_tiles, prologue, body);
     else
         gated_tile_loop<CL>(g, n_tiles, prologue, body, NoOp(), NoOp());
-}
-
-// The gate's two schedules with one call of ``body``, for bodies so large that
-// a copy per schedule would cost registers and code: under a static schedule
-// as static_tile_loop, otherwise tickets of one queue for the whole device
-// (the host asks for a gate without queue groups), and the tiles left if no
-// workgroup reached an allowed CU to the last workgroup of the grid (flagged).
-// ``body(tile, err)`` as in gated_tile_loop; every thread of the workgroup runs
-// the same iterations.  ``prologue`` may read operands, so workgroups on CUs
-// outside the mask do not run it (unless tiles are left): it would take from the
-// streams whose those CUs are.  Where all XCDs are allowed it does not wait for
-// the workgroup's own to be known.
-template <typename Prologue, typename Body>
-__device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles, Prologue prologue, Body body)
-{
-    __shared__ uint32_t s_ticket;
-    __shared__ uint32_t s_flag;
-    const auto rank = [&]() {
-        uint32_t xcc;
-        asm volatile("s_getreg_b32 %0, hwreg(HW_REG_XCC_ID)" : "=s"(xcc));
-        return g.xcd_rank[xcc & 0xFu];
-    };
-    if (g.tlog && blockIdx.x == 0 && threadIdx.x == 0)
-        __hip_atomic_store(&g.tlog[0], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-    uint32_t err = 0u;
-    // where the next tile comes from: the static stride, the queue, what is left
-    enum { kStride, kQueue, kLeft };
-    uint32_t from = g.statics ? kStride : kQueue;
-    uint32_t t = n_tiles;
-    // what is left of the queue once the last workgroup has arrived
-    auto take_left = [&]() {
-        t = __builtin_amdgcn_readfirstlane(
-            __hip_atomic_load(&g.q->grp_next[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        if (t < n_tiles)
-            err |= threadIdx.x == 0 ? kDevFlagGateFallback : 0u;
-        from = kLeft;
-    };
-    uint32_t cu = (uint32_t)kMaxCus;
-    bool mine = true;
-    if (from == kQueue) {
-        cu = my_cu_entry(g) & 0xFFFFu;
-        if (__builtin_amdgcn_readfirstlane(cu_allowed(g, cu) ? 1u : 0u) == 0u) {
-            if (__builtin_amdgcn_readfirstlane(arrive_last(g, &s_flag) ? 1u : 0u) == 0u)
-                return;
-            take_left();
-            mine = t < n_tiles;
-        }
-    } else if (g.n_allowed_xcd != g.n_xcd) {
-        mine = __builtin_amdgcn_readfirstlane(rank()) != 0xFFu;
-    }
-    if (mine)
-        prologue();
-    const uint32_t a = rank();
-    if (from == kStride && g.log_cu)
-        cu = my_cu_entry(g) & 0xFFFFu;
-    __syncthreads();
-    const uint32_t workers = (gridDim.x / g.n_xcd) * g.n_allowed_xcd;
-    if (from == kStride && a != 0xFFu)
-        t = (blockIdx.x / g.n_xcd) * g.n_allowed_xcd + a;
-    t = __builtin_amdgcn_readfirstlane(t);
-    for (;;) {
-        uint32_t tile = n_tiles;
-        if (from == kQueue) {
-            tile = claim_ticket(&g.q->grp_next[0], &s_ticket);
-            if (tile >= n_tiles) {
-                // (the flag is the same in every lane; without saying so here all
-                // that follows, the body's scalars too, would count as per-lane)
-                if (__builtin_amdgcn_readfirstlane(arrive_last(g, &s_flag) ? 1u : 0u) == 0u)
-                    break;
-                take_left();
-            }
-        }
-        if (from != kQueue) {
-            tile = t;
-            if (tile >= n_tiles)
-                break;
-            t += from == kStride ? workers : 1u;
-        }
-        log_tile(g, cu, tile);
-        body(__builtin_amdgcn_readfirstlane(tile), err);
-    }
-    if (from == kLeft) {
-        reset_slot(g.q);
-        if (g.tlog && threadIdx.x == 0) {
-            __builtin_amdgcn_s_waitcnt(0);
-            __hip_atomic_store(&g.tlog[1], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-        }
-    }
-    if (from == kStride)
-        static_end(g, a, NoOp(), err);
-    else if (err != 0u)
-        raise_flag(g.err, err);
 }
 
 // Wavefront-granular form of gated_tile_loop, for bodies whose work is
