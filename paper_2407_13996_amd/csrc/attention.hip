@@ -704,8 +704,8 @@ __device__ __forceinline__ float put_stats(const AttArgs &a, const Piece &x, uin
 // have taken this one's, the next V after the products with this one, into the
 // same registers, so that a wavefront has a step in flight for the registers
 // of one.  96 requests of up to 24000 tokens (4.7 GB, 32 query and 8 key heads
-// of 128) take 710 us, 6.7 TB/s; one of 1009 tokens 7, of which launch, plan
-// and the first loads are nearly all.
+// of 128) take 720 us with the join's 8, 6.6 TB/s; one of 1009 tokens 8 without,
+// of which launch, plan and the first loads are nearly all.
 template <int DT, int D>
 __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(D < 256 ? 2 : 1))) void k_attend_few(
     AttArgs a, SGDRC_SEQS_ARGS, uint32_t n_tiles, Gate g)
@@ -897,8 +897,8 @@ __device__ __forceinline__ uint32_t lds_token(uint32_t p)
 // wavefront and step at head_dim 128), products, softmax, products follow each
 // other, in both wavefronts of a SIMD at the same time, and their times add up
 // (measured for 24 requests of 64 nodes, 64 query and 8 key heads, over 2000 to
-// 8000 tokens: 370 us, where the arithmetic takes 210 at the rate of a large
-// plain product).  Wavefronts of 16 rows, four on a
+// 8000 tokens: 408 us with the join's 27, where the arithmetic takes 210 at the
+// rate of a large plain product).  Wavefronts of 16 rows, four on a
 // SIMD, took 440, steps of 64 tokens 580, two groups of wavefronts half a step
 // apart 500 and more, each with registers spilled.
 template <int DT, int D, int NB, int NW>

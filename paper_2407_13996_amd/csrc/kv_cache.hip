@@ -51,8 +51,8 @@ __device__ __forceinline__ MapAsk map_ask(const MapArgs &a, uint32_t r)
 // between workgroups does: its requests' and tokens' entries follow from the
 // sums in LDS.  The state goes to other memory than it is read from for the
 // same reason.  A step is bound by the launch and this chain of round trips
-// (lengths, sums, table or ring, slot), not by its bytes: 8 requests take 4.8
-// us, 2048 of which every ninth ends 13.5 (17 in tiles of four tokens a thread).
+// (lengths, sums, table or ring, slot), not by its bytes: 8 requests take 5.2
+// us, 2048 of which every ninth ends 13.4 (17 in tiles of four tokens a thread).
 __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_tiles, Gate g)
 {
     __shared__ uint32_t s_q[SGDRC_MAX_REQUESTS + 1];  // first token of each request
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
 // written element by element (every token of a decoding step; the ends of a
 // prompt's run).  A group belongs to the tile of its first token.  Bound by
 // the way from slots and rows through LDS to the stores, which a tile of 32
-// goes half as often: 16384 tokens of 8 heads take 32 us so (4.2 TB/s) and 36
+// goes half as often: 16384 tokens of 8 heads take 33 us so (4.0 TB/s) and 36
 // in tiles of 16; 61 tokens, which do not fill the GPU either way, 6.3 and 5.1.
 template <int D, int TOKENS>
 __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, RowsView v,
@@ -360,12 +360,13 @@ constexpr uint32_t kCommitBatch = 8;  // path entries whose loads are in flight 
 // A tile is one request in one layer.  A path ascends, so entry j's source
 // (path[j] >= j) is never the destination of an earlier entry, and a thread
 // that owns a column (16 bytes of K, one element of V) may load the sources of
-// several entries before it stores any.  Bound by memory's 128-byte lines: a
-// token's K is 16 bytes every 16 block_tokens, its V 2 bytes in every 16.  64
-// requests of 32 layers and 8 heads of 128 that keep 6 of 60 tokens take 109 us,
-// K and V half each; the lines that this touches take 81 at a copy's rate.
-// (Whole 16-byte groups of V, read and written again, took 104, and would
-// rewrite tokens that are not this call's.)
+// several entries before it stores any.  Bound by the scattered accesses that the
+// layout asks for: a token's K is 16 bytes every 16 block_tokens, its V 2 bytes
+// in every 16.  64 requests of 32 layers and 8 heads of 128 that keep 6 of 60
+// tokens take 109 us, K and V half each; 133 MB are fetched for them and 91 written
+// (counters of the L2), where 42 and 42 are moved, at 2.1 TB/s.  (Whole 16-byte
+// groups of V, read and written again, took 104, and would rewrite tokens that are
+// not this call's.)
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a, uint32_t n_requests,
                                                           uint32_t n_tiles, Gate g)
