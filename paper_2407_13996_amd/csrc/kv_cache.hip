@@ -46,13 +46,14 @@ __device__ __forceinline__ MapAsk map_ask(const MapArgs &a, uint32_t r)
     return q;
 }
 
-// Every workgroup adds up all requests for itself (three running sums: tokens,
-// wanted pages, returned pages), so that one launch without any exchange
-// between workgroups does: its requests' and tokens' entries follow from the
-// sums in LDS.  The state goes to other memory than it is read from for the
+// Every workgroup that may have a tile adds up all requests for itself (three
+// running sums: tokens, wanted pages, returned pages), so that one launch without any
+// exchange between workgroups does: its requests' and tokens' entries follow from
+// the sums in LDS.  The state goes to other memory than it is read from for the
 // same reason.  A step is bound by the launch and this chain of round trips
 // (lengths, sums, table or ring, slot), not by its bytes: 8 requests take 5.2
-// us, 2048 of which every ninth ends 13.4 (17 in tiles of four tokens a thread).
+// us, 2048 of which every ninth ends 13.4 (17 in tiles of four tokens a thread),
+// where a thread reads its 8 requests one after the other, and again for the sums.
 __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_tiles, Gate g)
 {
     __shared__ uint32_t s_q[SGDRC_MAX_REQUESTS + 1];  // first token of each request
