@@ -131,7 +131,6 @@ class Server:
         mask = torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in words], dtype=torch.int64,
                             device=DEV)
         self.totals, q_start, slots = self.map(new, n)
-        self.lens = torch.where(torch.tensor(new, device=DEV) < 0, 0, self.lens)   # ended
         at = self.lens.repeat_interleave(torch.tensor(counts, device=DEV)).long() + torch.tensor(depth, device=DEV)
         x = self.w.embed[tokens].float() + self.w.place[at].float()
         for layer in range(LAYERS):

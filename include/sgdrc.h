@@ -610,10 +610,12 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
  * blocks may name other requests' pages).  colored_kv_commit_within sees to that by
  * d_totals, the tokens in each request's cache with its draft (the lengths
  * that colored_kv_map wrote): the path is cut at the first token past them too,
- * so that a request that was not served keeps its length, and a total
- * below d_lens[r] or past the table's row accepts nothing; both raise
- * SGDRC_DEVERR_SEQ.  EINVAL: a bad cache, NULL or misaligned pointers,
- * path_stride outside 1..256, as colored_kv_map for the blocks. */
+ * so that a request that was not served keeps its length.  One whose total is
+ * below d_lens[r] has ended: it accepts nothing, and d_lens_out[r] becomes its
+ * total.  A path that is cut raises SGDRC_DEVERR_SEQ, as do totals below 0 or past
+ * the table's row, which accept nothing and leave the length.  EINVAL: a bad
+ * cache, NULL or misaligned pointers, path_stride outside 1..256, as
+ * colored_kv_map for the blocks. */
 int colored_kv_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks,
                       const int32_t *d_lens, const int32_t *d_path, uint32_t path_stride,
                       const int32_t *d_accepted, int32_t *d_lens_out, void *stream);
@@ -629,6 +631,8 @@ int colored_kv_commit_within(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const 
  * d_lens[r] + j by node i if bit j of node i's mask is set (d_mask: mask_words
  * 64-bit words for each token of q, bit j of a row in word j / 64) or, with
  * d_mask NULL, if j <= i: a chain, of which a single token is the shortest.
+ * Lengths of a request without nodes mean nothing (one that ends in this step
+ * has d_lens[r] tokens before it and none after).
  * Query head h reads key/value head h / (n_heads / kv_heads).  With
  *   s_ij = scale q_i . k_j, capped to softcap tanh(s_ij / softcap) if
  *   softcap > 0,

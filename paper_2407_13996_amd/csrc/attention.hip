@@ -89,8 +89,10 @@ __device__ __forceinline__ Req load_req(const AttArgs &a, const Seqs &sq, uint32
     q.nodes = min(end - q.start, a.max_nodes);
     q.total = total < 0 ? 0u : min((uint32_t)total, cap);
     q.ctx = ctx < 0 ? 0u : min((uint32_t)ctx, q.total);
-    q.ok = s <= e && e <= a.n_tokens && e - s <= a.max_nodes && total >= 0 && (uint32_t)total <= cap && ctx >= 0 &&
-           ctx <= total;
+    // lengths of a request without nodes are not used: one that ends in this step
+    // has its old length before it and none after
+    const bool lengths = total >= 0 && (uint32_t)total <= cap && ctx >= 0 && ctx <= total;
+    q.ok = s <= e && e <= a.n_tokens && e - s <= a.max_nodes && (s == e || lengths);
     return q;
 }
 

@@ -381,13 +381,14 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a
         const int32_t len = a.lens[r], want = a.accepted[r];
         const int32_t cap = (int32_t)(a.width << c.bshift);
         const int32_t total = a.totals ? a.totals[r] : cap;
-        const bool sound = len >= 0 && len <= total && total <= cap && want >= 0;
-        const uint32_t n = sound ? min((uint32_t)want, a.path_stride) : 0u;
+        const bool sound = len >= 0 && len <= cap && total >= 0 && total <= cap && want >= 0;
+        const bool ended = sound && total < len;
+        const uint32_t n = sound && !ended ? min((uint32_t)want, a.path_stride) : 0u;
         __syncthreads();  // the last tile's LDS is read
         if (threadIdx.x == 0u)
             s_n = n;
         __syncthreads();
-        uint32_t bad = !sound || (uint32_t)want > a.path_stride ? kDevErrSeq : 0u;
+        uint32_t bad = !sound || (uint32_t)want > (ended ? 0u : a.path_stride) ? kDevErrSeq : 0u;
         const uint32_t i = threadIdx.x;
         int32_t node = 0;
         if (i < n) {
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_commit(KvView c, CommitArgs a
         }
         err |= bad;
         if (layer == 0u && threadIdx.x == 0u)
-            a.lens_out[r] = sound ? len + (int32_t)good : len;
+            a.lens_out[r] = ended ? total : len + (int32_t)good;
         __syncthreads();
         uint8_t *const base = c.pool + layer * a.layer_stride;
         const uint32_t n_v = c.heads * (uint32_t)D, n_k = c.heads * (uint32_t)(D / 8);

@@ -91,7 +91,7 @@ def test_paths_are_cut_at_the_totals(ctx, layers):
     sg.colored_kv_commit(ctx, cache, i32(table), i32(lens), i32(path), i32(accepted), out, totals=i32(totals))
     commit_oracle(pool, layers, pages << (shift - 1), 1 << (shift - 1), block, heads, dim, table, lens, path, good)
     torch.cuda.synchronize()
-    assert out.tolist() == (lens + good).tolist()
+    assert out.tolist() == np.where((totals >= 0) & (totals < lens), totals, lens + good).tolist()
     assert torch.equal(d_pool.cpu(), pool)
     assert ctx.device_error() == sg.DEVERR_SEQ
     # all within: no flag, and the same as without totals
@@ -108,3 +108,41 @@ def test_paths_are_cut_at_the_totals(ctx, layers):
         assert out.tolist() == (lens + accepted).tolist()
         assert torch.equal(d_pool.cpu(), want)
         assert ctx.device_error() == 0
+
+
+def test_a_request_ends_in_a_step_of_others(ctx):
+    """Map, write, attend and commit with the state as it was before the step: the
+    request that ends has its old length before and none after, and raises nothing;
+    accepted tokens of it do."""
+    heads, dim, block, pages = 1, 64, 16, 8
+    elems, shift = ko.pages_of(heads, dim, block)
+    pool = torch.randn(pages << (shift - 1), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    d_pool = pool.to(DEV)
+    cache = cache_of(d_pool, pages, shift, block, heads, dim, sg.BF16)
+    s = State(ctx, 3, 3, pages, block)
+    s.lens, _ = s.map([40, 10, 5])
+    before = s.lens
+    totals, slots = s.map([-1, 3, 0])
+    assert totals.tolist() == [0, 13, 5]
+    rows = torch.randn(3, 2 * heads, dim, generator=torch.Generator().manual_seed(5)).to(torch.bfloat16)
+    q = rows.to(DEV)
+    sg.colored_kv_append(ctx, cache, 0, q[:, :1], q[:, 1:], slots)
+    out, lse = torch.zeros_like(q), torch.zeros(3, 2, device=DEV)
+    work = torch.empty(sg.tree_attention_workspace(cache, 2, 3), dtype=torch.uint8, device=DEV)
+    sg.colored_tree_attention(ctx, cache, 0, q, i32([0, 0, 3, 3]), s.table, before, totals, out, work, lse=lse, max_nodes=3,
+                              scale=0.125)
+    torch.cuda.synchronize()
+    assert ctx.device_error() == 0
+    at = s.table[1, 0].item() * block + np.arange(13)
+    flat, per = d_pool.cpu(), 1 << (shift - 1)
+    k, v = (ko.rows(flat, x, per, block, heads, dim, at) for x in (ko.k_index, ko.v_index))
+    seen = torch.ones(3, 13, dtype=torch.bool).tril(10)
+    o, ls, mass, dots = ko.attend(rows, k, v, seen, 0.125, 0.0)
+    ob, lb = ko.attend_bounds(torch.bfloat16, dim, 13, o, ls, mass, dots, 0.0)
+    assert bool(((out.cpu().double() - o).abs() <= ob).all()) and bool(((lse.cpu().double() - ls).abs() <= lb).all())
+    for first, flag in ((0, 0), (1, sg.DEVERR_SEQ)):
+        lens = i32([-1, -1, -1])
+        sg.colored_kv_commit(ctx, cache, s.table, before, i32([[0, 1], [0, 1], [0, 0]]), i32([first, 2, 0]), lens,
+                             totals=totals)
+        assert lens.tolist() == [0, 12, 5] and ctx.device_error() == flag
+    assert torch.equal(d_pool.cpu(), flat)
