@@ -484,6 +484,60 @@ int colored_gemv_form(uint32_t allowed_cus, uint32_t schedule, int w_dtype, uint
                       int x_dtype, uint32_t batch, uint32_t page_shift, uint32_t *form,
                       uint32_t *loads);
 
+/* ------------------------------------------------------- 4-bit weights
+ *
+ * A matrix whose element [m][k] is s[m][k / group] * (n[m][k] - z[m][k / group]):
+ * n a whole number 0..15, s and z of a 16-bit type, z 8 throughout where none
+ * are stored.  It lies in a paged tensor (sgdrc_paged), in this order:
+ *  - the codes n, in blocks of 16 rows by 128 columns, 1 KiB each, all blocks
+ *    of rows 0..15 first.  A block is [4][16 rows][16 bytes]: 32-bit word i of piece
+ *    [g][r] holds columns 32 i + 8 g .. + 7 of row r, column e of these eight
+ *    at bit 4 (e / 2 + 4 (e mod 2)).  (A piece is what one lane of a
+ *    matrix instruction takes, a block lies within a page whatever its size.)
+ *  - the scales s, for each block [4][128 / group][4 rows], row 4 i + j of the
+ *    block at [i][.][j];
+ *  - the zero points z likewise, if there are any.
+ * Rows and columns past the matrix are part of the blocks; their codes may be
+ * anything, their scales and zero points must be finite (colored_q4_pack writes 0). */
+#define SGDRC_MAX_Q4_BATCH 16
+typedef struct {
+    uint32_t rows;
+    uint32_t cols;   /* a multiple of group, at most 65536 */
+    uint32_t group;  /* columns with one scale: 32, 64 or 128 */
+    uint32_t dtype;  /* of scales, zero points and x: SGDRC_BF16 or SGDRC_F16 */
+    uint32_t zeros;  /* 1: zero points are stored */
+    uint32_t reserved; /* must be 0 */
+} sgdrc_q4;
+
+/* Bytes of the paged tensor (host-only, no context).  EINVAL: a bad
+ * description, NULL bytes. */
+int sgdrc_q4_bytes(const sgdrc_q4 *q, uint64_t *bytes);
+
+/* Lays a matrix out: d_codes holds a byte a code, row m at d_codes + m * code_stride
+ * (bytes); of a byte the lower 4 bits count.  d_scales and d_zeros (NULL
+ * unless q->zeros) are contiguous [rows][cols / group].  Every
+ * byte of the tensor is written (past the matrix with 0), none of its last page
+ * beyond it.  EINVAL: a bad description or paged tensor, page_shift outside [10, 30],
+ * NULL or misaligned pointers (2 bytes for scales and zero points), zero points given
+ * without q->zeros, code_stride below cols, 2^31 blocks or more. */
+int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q,
+                    const uint8_t *d_codes, uint64_t code_stride, const void *d_scales,
+                    const void *d_zeros, uint32_t page_shift, void *stream);
+
+/* colored_gemv for such a matrix: d_y[b * rows + m] = sum_k W[m][k] * x[b][k] for up to 16
+ * rows of x (contiguous [batch][cols] of q->dtype, 16-byte aligned), fp32 result.
+ * Products are of n + 16 with x, exact, and summed in fp32 within a group; what the
+ * offset adds, 24 times the sum of x over the group (16 + z where zero points are
+ * stored), is summed the same way and taken out, and the group's sum is scaled and
+ * added in fp32.  An infinity or NaN in row b of x therefore gives NaN in row b of y, and
+ * so may an element of x above 2^120.
+ * The order of all sums depends on the shape only, never on the CU mask: results
+ * are bitwise reproducible.  A block on a page outside the pool counts as zeros and
+ * raises SGDRC_DEVERR_PT_RANGE.  EINVAL: a bad description or paged tensor, page_shift
+ * outside [10, 30], batch outside 1..16, NULL or misaligned pointers. */
+int colored_gemv_q4(sgdrc_ctx *ctx, const sgdrc_paged *w, const sgdrc_q4 *q, const void *d_x,
+                    uint32_t batch, float *d_y, uint32_t page_shift, void *stream);
+
 /* ---------------------------------------------------- key/value cache
  *
  * The state of decoding on coloured pages.  A cache is a pool whose pages

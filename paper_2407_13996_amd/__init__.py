@@ -74,6 +74,11 @@ class RelayoutItem(ctypes.Structure):
                 ("page_shift", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
+class Q4(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("group", ctypes.c_uint32),
+                ("dtype", ctypes.c_uint32), ("zeros", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
 class KvCache(ctypes.Structure):
     _fields_ = [("pool", ctypes.c_void_p), ("pool_pages", ctypes.c_uint64), ("layer_stride", ctypes.c_uint64),
                 ("n_layers", ctypes.c_uint32), ("page_shift", ctypes.c_uint32), ("block_tokens", ctypes.c_uint32),
@@ -148,6 +153,9 @@ def lib() -> ctypes.CDLL:
             "colored_gemv": ([vp, P(Paged), i32, u32, u32, vp, i32, u32, vp, u32, vp], i32),
             "colored_gemv_plan": ([u32, i32, u32, u32, i32, u32, P(GemvPlan)], i32),
             "colored_gemv_form": ([u32, u32, i32, u32, u32, i32, u32, u32, P(u32), P(u32)], i32),
+            "sgdrc_q4_bytes": ([P(Q4), P(u64)], i32),
+            "colored_q4_pack": ([vp, P(Paged), P(Q4), vp, u64, vp, vp, u32, vp], i32),
+            "colored_gemv_q4": ([vp, P(Paged), P(Q4), vp, u32, vp, u32, vp], i32),
             "colored_kv_map": ([vp, u32, P(KvState), P(KvState), vp, u32, P(KvBlocks), vp, vp, vp, vp, vp, u32, vp],
                                i32),
             "colored_kv_append": ([vp, P(KvCache), u32, P(Rows), P(Rows), vp, u32, vp], i32),
@@ -483,6 +491,39 @@ def gemv_form(allowed_cus: int, schedule: str, w_dtype: int, M: int, K: int, x_d
                                    int(K), int(x_dtype), int(batch), int(page_shift), ctypes.byref(form),
                                    ctypes.byref(loads)))
     return ("tiles", "ring", "stream")[form.value], loads.value
+
+
+def q4(rows: int, cols: int, group: int, dtype: int, zeros: bool = False) -> Q4:
+    """Description of a matrix of 4-bit weights (sgdrc_q4): element [m][k] is
+    scale[m][k / group] * (code - zero[m][k / group]), zero 8 throughout where none
+    are stored; ``dtype`` (BF16 or F16) is that of scales, zero points and x."""
+    return Q4(int(rows), int(cols), int(group), int(dtype), int(bool(zeros)), 0)
+
+
+def q4_bytes(q: Q4) -> int:
+    """Bytes of the paged tensor that holds such a matrix (host-only; no device needed)."""
+    n = ctypes.c_uint64()
+    _check(lib().sgdrc_q4_bytes(q, n))
+    return n.value
+
+
+def colored_q4_pack(ctx, dst: Paged, q: Q4, codes, scales, zeros=None, page_shift: int = 16, stream=None) -> None:
+    """Lays a matrix out in the paged tensor ``dst``: ``codes`` [rows, cols], a byte
+    each (0..15), ``scales`` and ``zeros`` [rows, cols / group] of the matrix's dtype."""
+    if codes.shape != (q.rows, q.cols) or codes.element_size() != 1 or codes.stride(1) != 1:
+        raise ValueError(f"codes must be [{q.rows}, {q.cols}] bytes, rows without gaps inside")
+    for t, name in ((scales, "scales"), (zeros, "zeros")):
+        if t is not None and not (t.shape == (q.rows, q.cols // q.group) and _dtype_of(t) == q.dtype
+                                  and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous [{q.rows}, {q.cols // q.group}] of the matrix's dtype")
+    _check(lib().colored_q4_pack(_h(ctx), dst, q, _addr(codes), codes.stride(0) if q.rows > 1 else q.cols,
+                                 _addr(scales), _addr(zeros), int(page_shift), _stream(stream)))
+
+
+def colored_gemv_q4(ctx, w: Paged, q: Q4, x, batch: int, y, page_shift: int, stream=None) -> None:
+    """y[b] = W x[b] for ``batch`` rows (1..16) of x (contiguous [batch, cols] of the
+    matrix's dtype), y fp32 [batch, rows]."""
+    _check(lib().colored_gemv_q4(_h(ctx), w, q, _addr(x), int(batch), _addr(y), int(page_shift), _stream(stream)))
 
 
 def kv_cache(pool, pool_pages: int, page_shift: int, block_tokens: int, kv_heads: int, head_dim: int, dtype: int,

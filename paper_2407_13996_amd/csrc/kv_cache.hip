@@ -541,30 +541,11 @@ int check_rows(const sgdrc_rows *r, const char *name)
     return SGDRC_OK;
 }
 
-static int kv_layer(const sgdrc_kv_cache *c, uint32_t layer)
+int check_layer(const sgdrc_kv_cache *c, uint32_t layer)
 {
     if (layer >= c->n_layers)
         return set_error(SGDRC_EINVAL, "layer %u of %u", layer, c->n_layers);
     return SGDRC_OK;
-}
-
-// Launches kernel ``k`` of ``tiles`` tiles on the stream's allowed CUs.
-template <typename K, typename... A>
-static int launch_tiles(sgdrc_ctx *ctx, void *stream, uint64_t tiles, int occ, K k, A... args)
-{
-    Ctx *c = nullptr;
-    int rc = check_ctx(ctx, &c);
-    if (rc)
-        return rc;
-    Gate g;
-    LaunchInfo li;
-    rc = make_gate(c, stream, tiles, kStreamGroupCus, &g, &li, false, true);
-    if (rc)
-        return rc;
-    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(k, dim3(gated_grid(c, occ, tiles, li)), dim3(kKvThreads), 0, s, args..., (uint32_t)tiles, g);
-    SGDRC_HIP(hipGetLastError());
-    return finish_static_tlog(g, s);
 }
 
 // Tiles of 16 tokens as long as the GPU holds them all at once.
@@ -576,7 +557,7 @@ static int launch_append_tiles(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint
 {
     static const int occ = occupancy(k_kv_append<D, TOKENS>, kKvThreads);
     const uint64_t tiles = ((uint64_t)n_tokens + TOKENS - 1u) / TOKENS * cache->kv_heads;
-    return launch_tiles(ctx, stream, tiles, occ, k_kv_append<D, TOKENS>, kv_view(cache, layer), rows_view(k),
+    return launch_tiles(ctx, stream, tiles, occ, kKvThreads, k_kv_append<D, TOKENS>, kv_view(cache, layer), rows_view(k),
                         rows_view(v), slots, n_tokens);
 }
 
@@ -594,8 +575,8 @@ static int launch_commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const Comm
                          void *stream)
 {
     static const int occ = occupancy(k_kv_commit<D>, kKvThreads);
-    return launch_tiles(ctx, stream, (uint64_t)n_requests * cache->n_layers, occ, k_kv_commit<D>, kv_view(cache, 0), a,
-                        n_requests);
+    return launch_tiles(ctx, stream, (uint64_t)n_requests * cache->n_layers, occ, kKvThreads, k_kv_commit<D>, kv_view(cache, 0),
+                        a, n_requests);
 }
 
 static int commit(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, const sgdrc_kv_blocks *blocks, const int32_t *d_lens,
@@ -660,7 +641,7 @@ int colored_kv_map(sgdrc_ctx *ctx, uint32_t block_tokens, const sgdrc_kv_state *
     const uint64_t tiles = std::max<uint64_t>((blocks->n_requests + kMapTile - 1u) / kMapTile,
                                               ((uint64_t)n_tokens + kMapTile - 1u) / kMapTile);
     static const int occ = occupancy(k_kv_map, kKvThreads);
-    return launch_tiles(ctx, stream, tiles, occ, k_kv_map, a);
+    return launch_tiles(ctx, stream, tiles, occ, kKvThreads, k_kv_map, a);
 }
 
 int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer, const sgdrc_rows *k,
@@ -668,7 +649,7 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
 {
     clear_error();
     int rc = check_kv_cache(cache);
-    if (rc || (rc = kv_layer(cache, layer)))
+    if (rc || (rc = check_layer(cache, layer)))
         return rc;
     if (n_tokens > 0x7FFFFFFFu || (uint64_t)n_tokens * cache->kv_heads / 16u >= (1ull << 31) - 65536u)
         return set_error(SGDRC_EINVAL, "too many tokens");

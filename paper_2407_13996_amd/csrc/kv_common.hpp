@@ -141,8 +141,29 @@ __device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles
 
 int check_kv_cache(const sgdrc_kv_cache *c);
 int check_kv_blocks(const sgdrc_kv_blocks *b, uint32_t block_tokens);
+int check_layer(const sgdrc_kv_cache *c, uint32_t layer);
 int check_rows(const sgdrc_rows *r, const char *name);
 int check_aligned(const void *p, uint32_t bytes, const char *name);
+
+// Launches kernel ``k`` (a single_tile_loop of ``tiles`` tiles in workgroups of
+// ``threads``) on the stream's allowed CUs.
+template <typename K, typename... A>
+int launch_tiles(sgdrc_ctx *ctx, void *stream, uint64_t tiles, int occ, int threads, K k, A... args)
+{
+    Ctx *c = nullptr;
+    int rc = check_ctx(ctx, &c);
+    if (rc)
+        return rc;
+    Gate g;
+    LaunchInfo li;
+    rc = make_gate(c, stream, tiles, kStreamGroupCus, &g, &li, false, true);
+    if (rc)
+        return rc;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(k, dim3(gated_grid(c, occ, tiles, li)), dim3(threads), 0, s, args..., (uint32_t)tiles, g);
+    SGDRC_HIP(hipGetLastError());
+    return finish_static_tlog(g, s);
+}
 
 inline KvView kv_view(const sgdrc_kv_cache *c, uint32_t layer)
 {
