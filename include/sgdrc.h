@@ -44,8 +44,10 @@
  *  - A context serves one device.  It may be used from several host
  *    threads; operations on one stream are ordered, operations on different
  *    streams may run concurrently (each stream gets its own work queue).
- *  - The cache calls (colored_kv_map, colored_kv_append, colored_kv_commit,
- *    colored_kv_commit_within, colored_tree_attention) enqueue kernels only and may be captured too.
+ *  - The cache calls (colored_kv_map, colored_kv_append, colored_kv_append_rotated,
+ *    colored_kv_commit, colored_kv_commit_within, colored_tree_attention,
+ *    colored_draft_verify) and those of 4-bit weights (colored_q4_pack,
+ *    colored_gemv_q4) enqueue kernels only and may be captured too.
  *    What the host cannot know -- lengths, slots, block tables -- they read
  *    on the device and check there: what is out of range is skipped and
  *    raises SGDRC_DEVERR_SEQ (pages: SGDRC_DEVERR_PT_RANGE).
@@ -650,6 +652,39 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
                       const sgdrc_rows *k, const sgdrc_rows *v, const int64_t *d_slots,
                       uint32_t n_tokens, void *stream);
 
+/* What happens to queries and keys on their way to the attention.  A head h
+ * becomes h * rsqrt(mean(h^2) + eps) * w, element by element, if weights w are
+ * given (head_dim of them, of norm_dtype; q and k each have their own or none).
+ * Then its first rot_dims dimensions turn in pairs, by the angle position * freq[i] radians
+ * for pair i: (a, b) -> (a cos - b sin, a sin + b cos).  Pair i is
+ * dimensions (i, i + rot_dims / 2), or (2 i, 2 i + 1) if interleaved. */
+typedef struct {
+    const void *q_norm;   /* NULL: queries keep their length */
+    const void *k_norm;   /* NULL: keys do */
+    const float *freq;    /* rot_dims / 2 of them; NULL if rot_dims is 0 */
+    uint32_t norm_dtype;  /* SGDRC_F32, SGDRC_BF16 or SGDRC_F16 */
+    uint32_t rot_dims;    /* a multiple of 16, at most head_dim; 0: nothing turns */
+    uint32_t interleaved; /* 0 or 1 */
+    float eps;            /* not negative, finite */
+} sgdrc_rotation;
+
+/* colored_kv_append with norms and rotation of the keys on the way, and the same for
+ * the queries (n_heads heads each), which go to ``q_out``.  Token i turns by
+ * d_position[i] (colored_kv_map's for a chain; for a tree each node's depth added
+ * to its request's length); a token whose position is below 0 is left out: nothing of it is
+ * written.  Norms, angles and products are fp32 (angles taken from
+ * position * freq in 64 bits, so that far positions keep their fraction), rounded once to
+ * the cache's dtype.  K and V go to d_slots as in colored_kv_append; the queries of a token
+ * with slot -1 are written all the same.  q_out may be q itself; apart from that no
+ * rows that are written may share memory with each other or with rows that are read.
+ * n_tokens == 0 launches nothing.  EINVAL: as colored_kv_append; n_heads not a multiple
+ * of kv_heads or above 1024, a bad rotation, NULL or misaligned pointers. */
+int colored_kv_append_rotated(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t layer,
+                              const sgdrc_rows *q, uint32_t n_heads, const sgdrc_rows *q_out,
+                              const sgdrc_rows *k, const sgdrc_rows *v, const int64_t *d_slots,
+                              const int32_t *d_position, uint32_t n_tokens,
+                              const sgdrc_rotation *rotation, void *stream);
+
 /* Closes up the accepted path of each request's draft, in every layer: the
  * token at d_lens[r] + path[i] moves to d_lens[r] + i for i < d_accepted[r],
  * path = d_path + r * path_stride strictly ascending, from 0 on.  Then
@@ -722,6 +757,49 @@ int colored_tree_attention(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t
  * the number of requests (host-only, no context).  EINVAL: as there, NULL bytes. */
 int sgdrc_tree_attention_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads,
                                    uint32_t max_nodes, uint64_t *bytes);
+
+/* Verification of drafted trees against the target's probabilities, from given
+ * random numbers: which nodes a sampler of the target would have taken, and its
+ * next token.  Request r's nodes are rows d_q_start[r] .. d_q_start[r + 1] - 1 of all arrays, as
+ * for the attention; node 0 is the last token that the sequence has, node i > 0 has the
+ * token d_tokens[.] and the parent d_parents[.] (a node of the request, counted from its
+ * first, below i; the root's is not read).  Row i of target (``vocab`` probabilities, row t at
+ * d_target + t * target_stride elements) is the model's distribution after node i;
+ * row i of draft (nullable) the one that node i's children were drawn from,
+ * independently of each other.  Without draft the children are certain choices.
+ * At a node with rows p and q, c = 0 and S = 1, its children are looked at in
+ * order: one with token t and random number u is accepted if
+ * u q(t) S < max(p(t) - c q(t), 0), and the walk goes on at it; otherwise c
+ * becomes c + S, and S the sum of max(p - c q, 0).  (Without draft: accepted if
+ * u S < p(t), otherwise p(t) becomes 0 and S the sum of p.)  Where no child is
+ * left the next token is drawn from what is left there: the first v at which the
+ * running sum of max(p - c q, 0) passes u_0 times its total, u_0 the root's
+ * random number (from p itself, if nothing is left).  So the tokens are
+ * distributed as if drawn from the target alone.
+ * Sums are held in 64 bits.  Probabilities that are not positive (NaN too)
+ * count as 0, infinite ones as the largest fp32.  Random numbers lie in [0, 1); with
+ * others a token is chosen all the same.  A node whose token is outside the
+ * vocabulary, or whose parent is none of its request's nodes before it, is never accepted;
+ * the first raises SGDRC_DEVERR_SEQ if it is looked at.
+ * Request r's accepted nodes, the root first, go to d_path + r * path_stride (the rest of
+ * its path_stride entries become -1), their number to d_accepted[r], the next
+ * token to d_next[r]: what colored_kv_commit_within takes.  A walk ends where the path
+ * is full.  A request without nodes, or whose row of ``target`` holds nothing
+ * positive where the token is to be drawn (raises SGDRC_DEVERR_SEQ), gets d_next -1.
+ * d_lens and d_totals (nullable, both or none; lengths without and with the draft,
+ * as for the attention): a request whose total is below its length plus its nodes was not served,
+ * accepts nothing and gets -1.  max_nodes: no request has more nodes (those beyond are not looked
+ * at and raise SGDRC_DEVERR_SEQ, as do starts out of order or past n_tokens).  No output may share memory with
+ * an input.  EINVAL: dtype unknown, vocab 0 or above 2^31 - 1, strides below vocab or above
+ * 2^40, n_requests outside 1..4096, max_nodes or path_stride outside 1..256, NULL or misaligned pointers
+ * (rows: their elements). */
+int colored_draft_verify(sgdrc_ctx *ctx, uint32_t dtype, uint32_t vocab, const void *d_target,
+                         uint64_t target_stride, const void *d_draft, uint64_t draft_stride,
+                         const int32_t *d_tokens, const int32_t *d_parents, const float *d_uniform,
+                         uint32_t n_tokens, const uint32_t *d_q_start, uint32_t n_requests,
+                         uint32_t max_nodes, const int32_t *d_lens, const int32_t *d_totals,
+                         int32_t *d_path, uint32_t path_stride, int32_t *d_accepted, int32_t *d_next,
+                         void *stream);
 
 /* ---------------------------------------------------- bimodal tensors
  *

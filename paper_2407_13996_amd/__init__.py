@@ -94,6 +94,12 @@ class Rows(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
 
 
+class Rotation(ctypes.Structure):
+    _fields_ = [("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("freq", ctypes.c_void_p),
+                ("norm_dtype", ctypes.c_uint32), ("rot_dims", ctypes.c_uint32), ("interleaved", ctypes.c_uint32),
+                ("eps", ctypes.c_float)]
+
+
 class KvState(ctypes.Structure):
     _fields_ = [("ring_pos", ctypes.c_void_p), ("held", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
 
@@ -159,6 +165,10 @@ def lib() -> ctypes.CDLL:
             "colored_kv_map": ([vp, u32, P(KvState), P(KvState), vp, u32, P(KvBlocks), vp, vp, vp, vp, vp, u32, vp],
                                i32),
             "colored_kv_append": ([vp, P(KvCache), u32, P(Rows), P(Rows), vp, u32, vp], i32),
+            "colored_kv_append_rotated": ([vp, P(KvCache), u32, P(Rows), u32, P(Rows), P(Rows), P(Rows), vp, vp, u32,
+                                           P(Rotation), vp], i32),
+            "colored_draft_verify": ([vp, u32, u32, vp, u64, vp, u64, vp, vp, vp, u32, vp, u32, u32, vp, vp, vp, u32,
+                                      vp, vp, vp], i32),
             "colored_kv_commit": ([vp, P(KvCache), P(KvBlocks), vp, vp, u32, vp, vp, vp], i32),
             "colored_kv_commit_within": ([vp, P(KvCache), P(KvBlocks), vp, vp, vp, u32, vp, vp, vp], i32),
             "colored_tree_attention": ([vp, P(KvCache), u32, P(Rows), u32, vp, u32, u32, P(KvBlocks), vp, vp, vp, u32,
@@ -613,6 +623,71 @@ def colored_kv_append(ctx, cache: KvCache, layer: int, k, v, slots, stream=None)
                                    _rows(k, "k", cache.kv_heads, cache.head_dim, cache.dtype),
                                    _rows(v, "v", cache.kv_heads, cache.head_dim, cache.dtype),
                                    _ints_of(slots, "slots", 8), n, _stream(stream)))
+
+
+def colored_kv_append_rotated(ctx, cache: KvCache, layer: int, q, k, v, q_out, slots, position, freq=None,
+                              q_norm=None, k_norm=None, eps: float = 0.0, interleaved: bool = False,
+                              stream=None) -> None:
+    """colored_kv_append of k and v with, on the way, each head of q and k brought to
+    length sqrt(head_dim) (``q_norm``, ``k_norm``: weights [head_dim], None: not) and its
+    first 2 * len(``freq``) dimensions turned by position * freq (fp32, radians;
+    pairs of halves, or of neighbours if ``interleaved``).  q [tokens, heads, head_dim] goes to
+    ``q_out`` (which may be q).  ``position`` (int32): below 0, a token is left out."""
+    n, heads = slots.numel(), q.shape[1]
+    if not (q.shape[0] == k.shape[0] == v.shape[0] == position.numel() == n and q_out.shape == q.shape):
+        raise ValueError("q, k, v, q_out, slots and position must have as many tokens, q_out the heads of q")
+    norms = [t for t in (q_norm, k_norm) if t is not None]
+    for t in norms:
+        if not (_dtype_of(t) == _dtype_of(norms[0]) >= 0 and t.is_contiguous() and t.numel() == cache.head_dim):
+            raise ValueError("the norms' weights must be contiguous [head_dim], of one floating type")
+    if freq is not None and not (_dtype_of(freq) == F32 and freq.is_contiguous()):
+        raise ValueError("freq must be a contiguous fp32 tensor")
+    turn = Rotation(_addr(q_norm), _addr(k_norm), _addr(freq) if freq is not None and freq.numel() else None,
+                    _dtype_of(norms[0]) if norms else F32, 0 if freq is None else 2 * freq.numel(),
+                    int(bool(interleaved)), float(eps))
+    row = (cache.head_dim, cache.dtype)
+    _check(lib().colored_kv_append_rotated(_h(ctx), cache, int(layer), _rows(q, "q", heads, *row), heads,
+                                           _written_rows(q_out, "q_out", heads, *row),
+                                           _rows(k, "k", cache.kv_heads, *row), _rows(v, "v", cache.kv_heads, *row),
+                                           _ints_of(slots, "slots", 8), _ints_of(position, "position"), n, turn,
+                                           _stream(stream)))
+
+
+def colored_draft_verify(ctx, target, tokens, parents, uniform, q_start, path, accepted, next, draft=None, lens=None,
+                         totals=None, max_nodes: int = 256, stream=None) -> None:
+    """Which nodes of each request's tree a sampler of the target would have taken
+    (``path`` [requests, most], -1 past the ``accepted`` first) and its ``next`` token.
+    ``target`` and ``draft`` [tokens, vocab]: probabilities after each node, and those that
+    its children were drawn from (None: certain choices); ``tokens``, ``parents`` (in
+    the request's own count) and ``uniform`` (fp32, [0, 1)): an entry a node, the root's random
+    number is the next token's.  ``lens``, ``totals``: as for the attention; a
+    request that was not served accepts nothing.  path, accepted and lens, totals go on to colored_kv_commit."""
+    n, requests = tokens.numel(), q_start.numel() - 1
+    if not (target.dim() == 2 and target.shape[0] == n == parents.numel() == uniform.numel() and path.dim() == 2
+            and path.shape[0] == requests == accepted.numel() == next.numel()):
+        raise ValueError("the arrays' lengths do not fit the requests and their nodes")
+    if any(t is not None and t.numel() != requests for t in (lens, totals)):
+        raise ValueError("lens and totals must have an entry a request")
+    if draft is not None and not (draft.shape == target.shape and draft.dtype == target.dtype):
+        raise ValueError("draft must be as target")
+    for t in (target, draft):
+        if t is not None and t.numel() and t.stride(1) != 1 and t.shape[1] > 1:
+            raise ValueError("rows of probabilities must have no gaps inside")
+    if not (_dtype_of(uniform) == F32 and uniform.is_contiguous()):
+        raise ValueError("uniform must be a contiguous fp32 tensor")
+    if _dtype_of(target) < 0:
+        raise ValueError("probabilities must be fp32, bf16 or fp16")
+    vocab = target.shape[1]
+
+    def stride(t):
+        return vocab if t is None or n < 2 else t.stride(0)
+
+    _check(lib().colored_draft_verify(_h(ctx), _dtype_of(target), vocab, _addr(target), stride(target), _addr(draft),
+                                      stride(draft), _ints_of(tokens, "tokens"), _ints_of(parents, "parents"),
+                                      _addr(uniform), n, _ints_of(q_start, "q_start"), requests, int(max_nodes),
+                                      _ints_of(lens, "lens"), _ints_of(totals, "totals"), _ints_of(path, "path"),
+                                      path.shape[1], _ints_of(accepted, "accepted"), _ints_of(next, "next"),
+                                      _stream(stream)))
 
 
 def colored_kv_commit(ctx, cache: KvCache, table, lens, path, accepted, lens_out, stream=None, totals=None) -> None:

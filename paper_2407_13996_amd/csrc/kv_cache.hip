@@ -7,7 +7,6 @@
 
 namespace sgdrc {
 
-constexpr int kKvThreads = 256;
 constexpr uint32_t kMapTile = kKvThreads;  // requests and tokens of a map tile, one a thread
 constexpr uint32_t kRefused = 0xFFFFFFFFu;
 
@@ -221,10 +220,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_map(MapArgs a, uint32_t n_til
 }
 
 // A tile is TOKENS tokens of one head.  K goes to the cache as it comes, 16 bytes
-// at a time; V is turned, the 8 tokens of an aligned group of slots meeting
-// in one 16-byte store, through LDS.  Groups that the tokens do not fill are
-// written element by element (every token of a decoding step; the ends of a
-// prompt's run).  A group belongs to the tile of its first token.  Bound by
+// at a time; V is turned (ValueTurn).  Bound by
 // the way from slots and rows through LDS to the stores, which a tile of 32
 // goes half as often: 16384 tokens of 8 heads take 33 us so (4.0 TB/s) and 36
 // in tiles of 16; 61 tokens, which do not fill the GPU either way, 6.3 and 5.1.
@@ -233,14 +229,8 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
                                                           const int64_t *__restrict__ slots,
                                                           uint32_t n_tokens, uint32_t n_tiles, Gate g)
 {
-    constexpr int kRows = TOKENS + 7;                     // the tile's and those of a group that begins in it
     constexpr uint32_t V16 = D / 8;                       // 16-byte pieces of a row
-    constexpr uint32_t kBack = 7u;                        // tokens before the tile that are looked at
-    constexpr uint32_t kSeen = kBack + TOKENS + 7u;
-    __shared__ int64_t s_slot[kSeen];
-    __shared__ uint32_t s_bits[2];                        // leaders of full groups, single tokens
-    __shared__ uint32_t s_lead[TOKENS / 8 + 1];    // the leaders
-    __shared__ __attribute__((aligned(16))) uint16_t s_v[kRows][D + 8];
+    __shared__ ValueTurn<D, TOKENS> s;
     constexpr uint32_t kLoads = (TOKENS * V16 + kKvThreads - 1u) / kKvThreads;
     auto body = [&](uint32_t t, uint32_t &err) {
         const uint32_t h = t % c.heads, t0 = t / c.heads * (uint32_t)TOKENS;
@@ -262,88 +252,23 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvView c, RowsView k, 
             }
         }
         __syncthreads();  // the last tile's LDS is read
-        if (threadIdx.x < kSeen) {
-            const int64_t i = (int64_t)t0 + threadIdx.x - kBack;
-            int64_t s = i >= 0 && i < (int64_t)n_tokens ? slots[i] : -1;
-            if (s < -1 || (s >= 0 && ((uint64_t)s >> c.bshift) >= c.pool_pages)) {
-                err |= kDevErrSeq;
-                s = -1;
-            }
-            s_slot[threadIdx.x] = s;
-        }
+        s.take_slots(c, slots, nullptr, t0, n_tokens, err);
         __syncthreads();
-        if (threadIdx.x < 64u) {
-            // token ``threadIdx.x`` of the tile: does it lead a full group, or stand alone
-            bool lead = false, single = false;
-            if (threadIdx.x < (uint32_t)TOKENS) {
-                const uint32_t x = threadIdx.x + kBack;
-                const int64_t s = s_slot[x];
-                if (s >= 0) {
-                    const uint32_t in = (uint32_t)s & 7u;
-                    bool full = true;
-#pragma unroll
-                    for (uint32_t q = 0; q < 8u; ++q)
-                        full = full && s_slot[x - in + q] == s - (int64_t)in + (int64_t)q;
-                    lead = full && in == 0u;
-                    single = !full;
-                }
-            }
-            const uint64_t lb = __ballot(lead), sb = __ballot(single);
-            if (lead)
-                s_lead[__popcll(lb & ((1ull << threadIdx.x) - 1ull))] = threadIdx.x;
-            if (threadIdx.x == 0u) {
-                s_bits[0] = (uint32_t)lb;
-                s_bits[1] = (uint32_t)sb;
-            }
-        }
+        s.sort_out();
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) {
             const uint32_t i = j * kKvThreads + threadIdx.x;
             if (i < TOKENS * V16) {
-                const int64_t s = s_slot[kBack + k_tok(i)];
-                if (s >= 0) {
-                    uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
-                    *reinterpret_cast<u32x4 *>(at + k_off<D>(k_d8(i), (uint32_t)s & ((1u << c.bshift) - 1u), c.bshift)) = kk[j];
+                const int64_t at = s.slot[s.kBack + k_tok(i)];
+                if (at >= 0) {
+                    uint8_t *const to = c.pool + ((uint64_t)(at >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
+                    *reinterpret_cast<u32x4 *>(to + k_off<D>(k_d8(i), (uint32_t)at & ((1u << c.bshift) - 1u), c.bshift)) = kk[j];
                 }
-                *reinterpret_cast<u32x4 *>(&s_v[i / V16][(i % V16) * 8u]) = vv[j];
+                *reinterpret_cast<u32x4 *>(&s.v[i / V16][(i % V16) * 8u]) = vv[j];
             }
         }
         __syncthreads();
-        const uint32_t leaders = __builtin_amdgcn_readfirstlane(s_bits[0]);
-        const uint32_t singles = __builtin_amdgcn_readfirstlane(s_bits[1]);
-        // the rows past the tile of its last group (tokens that exist: their slots are consecutive)
-        if (leaders >> (TOKENS - 7)) {
-            const uint32_t last = 31u - (uint32_t)__builtin_clz(leaders);
-            const uint32_t n = (last + 8u - TOKENS) * V16;
-            for (uint32_t i = threadIdx.x; i < n; i += kKvThreads)
-                *reinterpret_cast<u32x4 *>(&s_v[TOKENS + i / V16][(i % V16) * 8u]) =
-                    *reinterpret_cast<const u32x4 *>(v.ptr + (uint64_t)(t0 + TOKENS + i / V16) * v.token +
-                                                     h * v.head + (i % V16) * 16u);
-            __syncthreads();
-        }
-        // a thread takes 16 bytes of a group: a dimension of its eight tokens
-        for (uint32_t i = threadIdx.x; i < (uint32_t)__builtin_popcount(leaders) * D; i += kKvThreads) {
-            const uint32_t x = s_lead[i / (uint32_t)D], d = i % (uint32_t)D;
-            const int64_t s = s_slot[kBack + x];
-            uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
-            const uint32_t t8 = ((uint32_t)s & ((1u << c.bshift) - 1u)) >> 3;
-            u32x4 o;
-#pragma unroll
-            for (uint32_t q = 0; q < 4u; ++q)
-                o[q] = (uint32_t)s_v[x + 2u * q][d] | ((uint32_t)s_v[x + 2u * q + 1u][d] << 16);
-            *reinterpret_cast<u32x4 *>(at + v_off<D>(t8, d, c.bshift)) = o;
-        }
-        if (singles) {
-            for (uint32_t i = threadIdx.x; i < (uint32_t)(TOKENS * D); i += kKvThreads) {
-                const uint32_t x = i / (uint32_t)D, d = i % (uint32_t)D;
-                if ((singles >> x) & 1u) {
-                    const int64_t s = s_slot[kBack + x];
-                    uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
-                    const uint32_t off = (uint32_t)s & ((1u << c.bshift) - 1u);
-                    *reinterpret_cast<uint16_t *>(at + v_off<D>(off >> 3, d, c.bshift) + (off & 7u) * 2u) = s_v[x][d];
-                }
-            }
-        }
+        s.write(c, v, t0, h);
     };
     single_tile_loop(g, n_tiles, NoOp(), body);
 }

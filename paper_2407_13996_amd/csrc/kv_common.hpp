@@ -1,5 +1,5 @@
 // What the paged key/value cache's kernels share: where a token's elements lie,
-// the loop over tiles, and the host's checks of caches, block tables and rows.
+// how V is turned, the loop over tiles, and the host's checks of caches, block tables and rows.
 #pragma once
 
 #include "host_common.hpp"
@@ -44,6 +44,112 @@ __device__ __forceinline__ uint32_t head_bytes(uint32_t bshift)
 {
     return (uint32_t)D * 4u << bshift;
 }
+
+constexpr int kKvThreads = 256;
+
+// LDS of a workgroup of kKvThreads that writes V of TOKENS tokens of one head.  V is
+// turned on the way: the 8 tokens of an aligned group of slots meet in one
+// 16-byte store.  Groups that the tokens do not fill are
+// written element by element (every token of a decoding step; the ends of a
+// prompt's run).  A group belongs to the tile of its first token.
+template <int D, int TOKENS>
+struct ValueTurn {
+    static constexpr uint32_t kRows = TOKENS + 7;         // the tile's and those of a group that begins in it
+    static constexpr uint32_t V16 = D / 8;                // 16-byte pieces of a row
+    static constexpr uint32_t kBack = 7u;                 // tokens before the tile that are looked at
+    static constexpr uint32_t kSeen = kBack + TOKENS + 7u;
+    int64_t slot[kSeen];
+    uint32_t bits[2];                                     // leaders of full groups, single tokens
+    uint32_t lead[TOKENS / 8 + 1];                        // the leaders
+    __attribute__((aligned(16))) uint16_t v[kRows][D + 8];
+
+    // The slots of the tile's tokens and those around it, -1 past the ends, for slots
+    // out of range (flagged) and, if ``position`` is given, where that is below 0.
+    __device__ __forceinline__ void take_slots(const KvView &c, const int64_t *slots, const int32_t *position,
+                                               uint32_t t0, uint32_t n_tokens, uint32_t &err)
+    {
+        if (threadIdx.x < kSeen) {
+            const int64_t i = (int64_t)t0 + threadIdx.x - kBack;
+            const bool in = i >= 0 && i < (int64_t)n_tokens;
+            int64_t s = in ? slots[i] : -1;
+            if (position && in && position[i] < 0)
+                s = -1;
+            if (s < -1 || (s >= 0 && ((uint64_t)s >> c.bshift) >= c.pool_pages)) {
+                err |= kDevErrSeq;
+                s = -1;
+            }
+            slot[threadIdx.x] = s;
+        }
+    }
+
+    // Which tokens lead a full group, which stand alone (after a barrier).
+    __device__ __forceinline__ void sort_out()
+    {
+        if (threadIdx.x < 64u) {
+            bool leads = false, single = false;
+            if (threadIdx.x < (uint32_t)TOKENS) {
+                const uint32_t x = threadIdx.x + kBack;
+                const int64_t s = slot[x];
+                if (s >= 0) {
+                    const uint32_t in = (uint32_t)s & 7u;
+                    bool full = true;
+#pragma unroll
+                    for (uint32_t q = 0; q < 8u; ++q)
+                        full = full && slot[x - in + q] == s - (int64_t)in + (int64_t)q;
+                    leads = full && in == 0u;
+                    single = !full;
+                }
+            }
+            const uint64_t lb = __ballot(leads), sb = __ballot(single);
+            if (leads)
+                lead[__popcll(lb & ((1ull << threadIdx.x) - 1ull))] = threadIdx.x;
+            if (threadIdx.x == 0u) {
+                bits[0] = (uint32_t)lb;
+                bits[1] = (uint32_t)sb;
+            }
+        }
+    }
+
+    // The stores, with the tile's rows in ``v`` (after another barrier).
+    __device__ __forceinline__ void write(const KvView &c, const RowsView &from, uint32_t t0, uint32_t h)
+    {
+        const uint32_t leaders = __builtin_amdgcn_readfirstlane(bits[0]);
+        const uint32_t singles = __builtin_amdgcn_readfirstlane(bits[1]);
+        // the rows past the tile of its last group (tokens that exist: their slots are consecutive)
+        if (leaders >> (TOKENS - 7)) {
+            const uint32_t last = 31u - (uint32_t)__builtin_clz(leaders);
+            const uint32_t n = (last + 8u - TOKENS) * V16;
+            for (uint32_t i = threadIdx.x; i < n; i += kKvThreads)
+                *reinterpret_cast<u32x4 *>(&v[TOKENS + i / V16][(i % V16) * 8u]) =
+                    *reinterpret_cast<const u32x4 *>(from.ptr + (uint64_t)(t0 + TOKENS + i / V16) * from.token +
+                                                     h * from.head + (i % V16) * 16u);
+            __syncthreads();
+        }
+        // a thread takes 16 bytes of a group: a dimension of its eight tokens
+        for (uint32_t i = threadIdx.x; i < (uint32_t)__builtin_popcount(leaders) * D; i += kKvThreads) {
+            const uint32_t x = lead[i / (uint32_t)D], d = i % (uint32_t)D;
+            const int64_t s = slot[kBack + x];
+            uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
+            const uint32_t t8 = ((uint32_t)s & ((1u << c.bshift) - 1u)) >> 3;
+            u32x4 o;
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q)
+                o[q] = (uint32_t)v[x + 2u * q][d] | ((uint32_t)v[x + 2u * q + 1u][d] << 16);
+            *reinterpret_cast<u32x4 *>(at + v_off<D>(t8, d, c.bshift)) = o;
+        }
+        if (singles) {
+            for (uint32_t i = threadIdx.x; i < (uint32_t)(TOKENS * D); i += kKvThreads) {
+                const uint32_t x = i / (uint32_t)D, d = i % (uint32_t)D;
+                if ((singles >> x) & 1u) {
+                    const int64_t s = slot[kBack + x];
+                    uint8_t *const at = c.pool + ((uint64_t)(s >> c.bshift) << c.shift) + h * head_bytes<D>(c.bshift);
+                    const uint32_t off = (uint32_t)s & ((1u << c.bshift) - 1u);
+                    *reinterpret_cast<uint16_t *>(at + v_off<D>(off >> 3, d, c.bshift) + (off & 7u) * 2u) = v[x][d];
+                }
+            }
+        }
+    }
+};
 
 // The gate's two schedules with one call of ``body``, for bodies so large that
 // a copy per schedule would cost registers and code: under a static schedule
