@@ -503,7 +503,7 @@ int colored_gemv_form(uint32_t allowed_cus, uint32_t schedule, int w_dtype, uint
  * anything, their scales and zero points must be finite (colored_q4_pack writes 0). */
 #define SGDRC_MAX_Q4_BATCH 16
 typedef struct {
-    uint32_t rows;
+    uint32_t rows;   /* with cols: below 2^26 blocks (64 GiB of codes) */
     uint32_t cols;   /* a multiple of group, at most 65536 */
     uint32_t group;  /* columns with one scale: 32, 64 or 128 */
     uint32_t dtype;  /* of scales, zero points and x: SGDRC_BF16 or SGDRC_F16 */
@@ -521,7 +521,7 @@ int sgdrc_q4_bytes(const sgdrc_q4 *q, uint64_t *bytes);
  * byte of the tensor is written (past the matrix with 0), none of its last page
  * beyond it.  EINVAL: a bad description or paged tensor, page_shift outside [10, 30],
  * NULL or misaligned pointers (2 bytes for scales and zero points), zero points given
- * without q->zeros, code_stride below cols, 2^31 blocks or more. */
+ * without q->zeros, code_stride below cols. */
 int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q,
                     const uint8_t *d_codes, uint64_t code_stride, const void *d_scales,
                     const void *d_zeros, uint32_t page_shift, void *stream);

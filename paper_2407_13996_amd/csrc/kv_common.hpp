@@ -245,6 +245,95 @@ __device__ __forceinline__ void single_tile_loop(const Gate &g, uint32_t n_tiles
         raise_flag(g.err, err);
 }
 
+// The same for bodies that load on into the workgroup's next tiles:
+// ``prime(tile, next)`` starts the loads of the first, ``body(tile, next, after, err)``
+// works on a tile whose loads are under way and starts those of the two that it
+// takes after it (n_tiles or more: none; the queue's tickets are taken ahead for that).
+// The body holds a barrier.
+template <typename Prime, typename Prologue, typename Body>
+__device__ __forceinline__ void single_tile_stream(const Gate &g, uint32_t n_tiles, Prime prime, Prologue prologue,
+                                                   Body body)
+{
+    __shared__ uint32_t s_ticket;
+    __shared__ uint32_t s_flag;
+    uint32_t xcc;
+    asm volatile("s_getreg_b32 %0, hwreg(HW_REG_XCC_ID)" : "=s"(xcc));
+    const uint32_t a = g.xcd_rank[xcc & 0xFu];
+    if (g.tlog && blockIdx.x == 0 && threadIdx.x == 0)
+        __hip_atomic_store(&g.tlog[0], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    uint32_t err = 0u;
+    const uint32_t workers = (gridDim.x / g.n_xcd) * g.n_allowed_xcd;
+    const bool queue = g.statics == 0u;
+    uint32_t cu = queue || g.log_cu ? my_cu_entry(g) & 0xFFFFu : (uint32_t)kMaxCus;
+    uint32_t t = n_tiles, next = n_tiles, after = n_tiles, step = workers;
+    bool left = false;  // working on what the queue has left
+    if (!queue) {
+        if (a != 0xFFu) {
+            t = (blockIdx.x / g.n_xcd) * g.n_allowed_xcd + a;
+            next = t + workers;
+            after = next + workers;
+        }
+    } else if (__builtin_amdgcn_readfirstlane(cu_allowed(g, cu) ? 1u : 0u)) {
+        t = claim_ticket(&g.q->grp_next[0], &s_ticket);
+        next = claim_ticket(&g.q->grp_next[0], &s_ticket);
+        after = claim_ticket(&g.q->grp_next[0], &s_ticket);
+    }
+    bool fresh = true;
+    for (;;) {
+        t = __builtin_amdgcn_readfirstlane(t);
+        next = __builtin_amdgcn_readfirstlane(next);
+        after = __builtin_amdgcn_readfirstlane(after);
+        if (queue && !left && t >= n_tiles) {
+            if (__builtin_amdgcn_readfirstlane(arrive_last(g, &s_flag) ? 1u : 0u) == 0u)
+                break;
+            // the last workgroup of the grid
+            left = fresh = true;
+            step = 1u;
+            t = __builtin_amdgcn_readfirstlane(
+                __hip_atomic_load(&g.q->grp_next[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            next = t + 1u;
+            after = t + 2u;
+            if (t < n_tiles)
+                err |= threadIdx.x == 0 ? kDevFlagGateFallback : 0u;
+        }
+        if (t >= n_tiles)
+            break;
+        if (fresh) {
+            prime(t, next);
+            prologue();
+            __syncthreads();
+            fresh = false;
+        }
+        uint32_t ahead = 0u;
+        if (queue && !left && threadIdx.x == 0)
+            ahead = __hip_atomic_fetch_add(&g.q->grp_next[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        log_tile(g, cu, t);
+        body(t, next, after, err);
+        t = next;
+        next = after;
+        if (queue && !left) {
+            if (threadIdx.x == 0)
+                s_ticket = ahead;
+            __syncthreads();
+            after = s_ticket;
+        } else {
+            after += step;
+        }
+    }
+    if (left) {
+        reset_slot(g.q);
+        if (g.tlog && threadIdx.x == 0) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __hip_atomic_store(&g.tlog[1], __builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (!queue)
+        static_end(g, a, NoOp(), err);
+    else if (err != 0u)
+        raise_flag(g.err, err);
+}
+
 int check_kv_cache(const sgdrc_kv_cache *c);
 int check_kv_blocks(const sgdrc_kv_blocks *b, uint32_t block_tokens);
 int check_layer(const sgdrc_kv_cache *c, uint32_t layer);

@@ -14,7 +14,7 @@
 // (four of its rows in a lane) is scaled in fp32.
 #include <algorithm>
 
-#include "host_common.hpp"
+#include "kv_common.hpp"
 
 namespace sgdrc {
 
@@ -29,9 +29,8 @@ constexpr uint32_t kQ4Outside = 0xFFFFFFF0u;  // an offset past any buffer resou
 
 struct Q4View {
     const uint8_t *pool;
-    const uint32_t *pt;
     uint64_t pool_pages;
-    uint64_t scales, zeros;  // where they begin in the tensor
+    uint32_t scales, zeros;  // where they begin in the tensor, in 32 bytes
     uint32_t shift;
     uint32_t rows, cols, segs;
 };
@@ -47,12 +46,15 @@ __device__ __forceinline__ f32x4 q4_mfma(u32x4 a, u32x4 b, f32x4 c)
                                                       0, 0);
 }
 
-// Eight codes of a word as 16 + n, columns in order.
+// Eight codes of a word as 16 + n, columns in order; ``one`` is q4_one in a
+// vector register (an instruction takes one constant from elsewhere).
 template <int DT>
-__device__ __forceinline__ u32x4 q4_codes(uint32_t w)
+constexpr uint32_t q4_one = DT == SGDRC_BF16 ? 0x41804180u : 0x4C004C00u;  // 16, twice
+
+template <int DT>
+__device__ __forceinline__ u32x4 q4_codes(uint32_t w, uint32_t one)
 {
-    constexpr uint32_t one = DT == SGDRC_BF16 ? 0x41804180u : 0x4C004C00u;  // 16, twice
-    constexpr int at = DT == SGDRC_BF16 ? 3 : 6;                            // of the lowest free mantissa bit
+    constexpr int at = DT == SGDRC_BF16 ? 3 : 6;  // of the lowest free mantissa bit
     constexpr uint32_t field = 0x000F000Fu << at;
     u32x4 a;
     a.x = ((w << at) & field) | one;
@@ -62,111 +64,255 @@ __device__ __forceinline__ u32x4 q4_codes(uint32_t w)
     return a;
 }
 
-// Two numbers of 16 bits.
+// Eight numbers of 16 bits as fp32.
 template <int DT>
-__device__ __forceinline__ void q4_pair(uint32_t w, float &lo, float &hi)
+__device__ __forceinline__ void q4_widen(u32x4 w, f32x4 &lo, f32x4 &hi)
 {
-    if (DT == SGDRC_BF16) {
-        lo = __uint_as_float(w << 16);
-        hi = __uint_as_float(w & 0xFFFF0000u);
-    } else {
-        const f16x2 v = __builtin_bit_cast(f16x2, w);
-        lo = (float)v.x;
-        hi = (float)v.y;
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (DT == SGDRC_BF16) {
+            f[2 * i] = __uint_as_float(x[i] << 16);
+            f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        } else {
+            const f16x2 v = __builtin_bit_cast(f16x2, x[i]);
+            f[2 * i] = (float)v.x;
+            f[2 * i + 1] = (float)v.y;
+        }
     }
+    lo = f32x4{f[0], f[1], f[2], f[3]};
+    hi = f32x4{f[4], f[5], f[6], f[7]};
 }
 
-// A tile is a block of 16 rows; its columns' segments are shared out to the
-// workgroup's wavefronts in contiguous runs, whose sums are added in wave order.
-template <int DT, int PER, bool ZEROS>
-__global__ __launch_bounds__(kQ4Threads) void k_gemv_q4(Q4View v, const uint8_t *__restrict__ x, uint32_t batch,
-                                                        float *__restrict__ y, uint32_t n_tiles, Gate g)
+// R blocks of rows a tile.  The segments of the columns are shared out to the
+// workgroup's wavefronts in runs of ``run``, whose sums are added in wave order; a
+// wavefront goes through its run in units of NS = 4 / R segments, R x NS blocks.  A
+// unit's codes (4 KiB) and scales are in flight while the one before is worked on, a
+// register of codes is loaded again as soon as it is used, over the ends of tiles
+// too; the page-table entries are gathered a unit ahead of that.  x is in LDS in the
+// order of the operands (XL), or comes from the L2 a segment ahead.
+template <int DT, int PER, bool ZEROS, int R, bool XL>
+__global__ __launch_bounds__(kQ4Threads) __attribute__((amdgpu_waves_per_eu(4))) void k_gemv_q4(
+    Q4View v, const uint32_t *__restrict__ pt, const uint8_t *__restrict__ x, uint32_t batch, uint32_t run,
+    float *__restrict__ y, uint32_t n_tiles, Gate g)
 {
-    constexpr uint32_t kScaleBlock = PER * 32u;
-    constexpr int SW = 2 * PER;  // words of scales a lane takes
-    __shared__ f32x4 s_red[kQ4Waves][64];
+    constexpr int NS = 4 / R;
+    constexpr int PLANES = ZEROS ? 2 : 1;
+    constexpr uint32_t PIECES = 2u * PER;       // of 16 bytes, of a block's scales
+    constexpr uint32_t PLANE = 4u * PIECES;     // lanes that fetch a unit's scales
+    constexpr uint32_t RB = R == 4 ? 1 : 2;     // buffers of partial sums
+    __shared__ f32x4 s_red[RB][kQ4Waves][R][64];
+    __shared__ f32x4 s_sc[kQ4Waves][PLANES * PLANE * 2];  // of a unit, fp32: [plane][block][4][PER]
+    extern __shared__ u32x4 s_x[];              // [segment][step][4][batch]
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     const uint32_t col = lane & 15u, grp = lane >> 4;
     const uint32_t x_row = v.cols * 2u;
-    const uint64_t pmask = (1ull << v.shift) - 1ull;
-    const Rsrc xr = make_rsrc(x, batch * x_row);
     const uint32_t x_at = col < batch ? col * x_row + grp * 16u : kQ4Outside;
-    const uint32_t s0 = v.segs * wave / (uint32_t)kQ4Waves, s1 = v.segs * (wave + 1u) / (uint32_t)kQ4Waves;
+    const uint32_t x_lds = grp * batch + min(col, batch - 1u);
+    const uint32_t first = wave * run, units = (run + NS - 1u) / NS;
+    const uint32_t mine = min(run, v.segs > first ? v.segs - first : 0u);  // segments of the wavefront
+    const uint32_t row_blocks = (v.rows + 15u) / 16u;
     // the offset's operand: -24 in both types, or -1 where the zero point comes with the group
     constexpr uint32_t kOff = ZEROS ? (DT == SGDRC_BF16 ? 0xBF80BF80u : 0xBC00BC00u)
                                     : (DT == SGDRC_BF16 ? 0xC1C0C1C0u : 0xCE00CE00u);
-    const u32x4 off = {kOff, kOff, kOff, kOff};
-    auto body = [&](uint32_t t, uint32_t, uint32_t &err, auto &&) {
-        f32x4 total = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t s = s0; s < s1; ++s) {
-            const uint64_t block = (uint64_t)t * v.segs + s;
-            auto at = [&](uint64_t byte, uint32_t &e) {
-                e = __builtin_amdgcn_readfirstlane(checked_page(v.pt, byte >> v.shift, v.pool_pages, err));
-                return v.pool + ((uint64_t)e << v.shift) + (byte & pmask);
-            };
-            uint32_t ec, es, ez = 0u;
-            const uint8_t *const pc = at(block * kQ4Block, ec);
-            const uint8_t *const ps = at(v.scales + block * kScaleBlock, es);
-            const uint8_t *const pz = ZEROS ? at(v.zeros + block * kScaleBlock, ez) : ps;
-            const bool ok = ec != kBadPage && es != kBadPage && ez != kBadPage;
-            const u32x4 w = buf_load_nt(make_rsrc(pc, ok ? kQ4Block : 0u), lane * 16u);
-            uint32_t sc[SW], zp[SW];
-            const Rsrc rs = make_rsrc(ps, ok ? kScaleBlock : 0u), rz = make_rsrc(pz, ok ? kScaleBlock : 0u);
-#pragma unroll
-            for (int i = 0; i < SW; ++i) {
-                sc[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, grp * (uint32_t)SW * 4u + i * 4u, 0, kAuxNt);
-                zp[i] = ZEROS ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rz, grp * (uint32_t)SW * 4u + i * 4u, 0, kAuxNt) : 0u;
-            }
-            u32x4 xb[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                xb[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                    xr, s * 128u + 32u * i < v.cols ? x_at + (s * 128u + 32u * i) * 2u : kQ4Outside, 0, 0));
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-            constexpr int kSteps = 4 / PER;
-#pragma unroll
-            for (int p = 0; p < PER; ++p) {
-                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int i = p * kSteps; i < (p + 1) * kSteps; ++i)
-                    o = q4_mfma<DT>(off, xb[i], o);
-                f32x4 acc = ZEROS ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : o;
-#pragma unroll
-                for (int i = p * kSteps; i < (p + 1) * kSteps; ++i)
-                    acc = q4_mfma<DT>(q4_codes<DT>(ww[i]), xb[i], acc);
-                float f[4], z[4];
-                q4_pair<DT>(sc[2 * p], f[0], f[1]);
-                q4_pair<DT>(sc[2 * p + 1], f[2], f[3]);
-                if (ZEROS) {
-                    q4_pair<DT>(zp[2 * p], z[0], z[1]);
-                    q4_pair<DT>(zp[2 * p + 1], z[2], z[3]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float a = ZEROS ? __builtin_fmaf(z[j] + 16.0f, o[j], acc[j]) : acc[j];
-                    total[j] = __builtin_fmaf(f[j], a, total[j]);
-                }
-            }
-        }
-        s_red[wave][lane] = total;
-        __syncthreads();
-        if (wave == 0u) {
-            f32x4 r = s_red[0][lane];
-#pragma unroll
-            for (int i = 1; i < kQ4Waves; ++i)
-                r += s_red[i][lane];
-            if (col < batch) {
-#pragma unroll
-                for (uint32_t j = 0; j < 4u; ++j) {
-                    const uint32_t m = t * 16u + grp * 4u + j;
-                    if (m < v.rows)
-                        y[(uint64_t)col * v.rows + m] = r[j];
-                }
-            }
-        }
-        __syncthreads();
+    uint32_t off_word = kOff, one = q4_one<DT>;
+    asm volatile("" : "+v"(off_word), "+v"(one));
+    const u32x4 off = {off_word, off_word, off_word, off_word};
+    uint32_t bad = 0u;
+    // A lane looks up the page of block ``my_code`` of a unit, and has one piece of the
+    // scales: of a plane, of a block, from a byte of it on.
+    const uint32_t my_code = lane & 3u, my_plane = lane / PLANE, my_block = lane % PLANE / PIECES;
+    const uint32_t code_row = my_code / NS, code_seg = my_code % NS, sc_row = my_block / NS, sc_seg = my_block % NS;
+    const uint32_t code_off = code_row * v.segs + code_seg, sc_off = sc_row * v.segs + sc_seg;
+    const uint32_t sc_base = my_plane ? v.zeros : v.scales, sc_byte = lane % PIECES * 16u;
+    const uint32_t low10 = (1u << (v.shift - 10u)) - 1u, low5 = (1u << (v.shift - 5u)) - 1u;
+
+    u32x4 w[R][NS];   // a unit's codes
+    u32x4 sc;         // this lane's piece of its scales
+    u32x4 xs[2][4];   // x of a segment and of the next
+
+    // A unit: its first block, how many row blocks and segments of it there are, and
+    // this lane's page-table entries as the table holds them.
+    struct Unit {
+        uint32_t block, rows, segs, code_page, sc_page;
     };
-    tile_loop<Claim::Ahead>(g, n_tiles, NoOp(), body);
+    auto unit_of = [&](uint32_t t, uint32_t u) __attribute__((always_inline)) {
+        Unit d;
+        const uint32_t rb = t * R, s = u * NS;
+        const bool in = (t < n_tiles) & (s < mine);
+        d.rows = in ? min(row_blocks - rb, (uint32_t)R) : 0u;
+        d.segs = in ? min(mine - s, (uint32_t)NS) : 0u;
+        d.block = in ? rb * v.segs + first + s : 0u;
+        // (a block that is not there: the first)
+        const uint32_t code = d.block + (code_row < d.rows && code_seg < d.segs ? code_off : 0u);
+        const uint32_t scale = d.block + (sc_row < d.rows && sc_seg < d.segs ? sc_off : 0u);
+        d.code_page = pt[code >> (v.shift - 10u)];
+        d.sc_page = pt[(sc_base + scale * PER) >> (v.shift - 5u)];
+        return d;
+    };
+    auto load_codes = [&](const Unit &d, int b) __attribute__((always_inline)) {
+        const uint32_t page = __builtin_amdgcn_readlane(d.code_page, b);
+        const uint32_t r = b / NS, i = b % NS;
+        const bool ok = r < d.rows && i < d.segs && page < v.pool_pages;
+        const uint8_t *const at = v.pool + ((uint64_t)page << v.shift) + (((d.block + r * v.segs + i) & low10) << 10);
+        w[r][i] = buf_load_nt(make_rsrc(at, ok ? kQ4Block : 0u), lane * 16u);
+    };
+    auto load_scales = [&](const Unit &d) __attribute__((always_inline)) {
+        // (a block without codes, or without one of its planes, has no scales)
+        const bool code_in = code_row < d.rows && code_seg < d.segs;
+        const bool sc_in = sc_row < d.rows && sc_seg < d.segs && my_plane < (uint32_t)PLANES;
+        const bool code_ok = d.code_page < v.pool_pages, sc_ok = d.sc_page < v.pool_pages;
+        bad |= (code_in && !code_ok) || (sc_in && !sc_ok) ? kDevErrPtRange : 0u;
+        const uint32_t codes_there = (uint32_t)__ballot(code_ok);
+        bool ok = sc_in && sc_ok && ((codes_there >> my_block) & 1u);
+        if (ZEROS) {
+            const uint64_t planes_there = __ballot(sc_ok);
+            ok = ok && ((planes_there >> (my_block * PIECES)) & 1ull) &&
+                 ((planes_there >> (PLANE % 64u + my_block * PIECES)) & 1ull);
+        }
+        sc = u32x4{0u, 0u, 0u, 0u};
+        if (ok)
+            sc = load_nt(v.pool + ((uint64_t)d.sc_page << v.shift) +
+                         ((((sc_base + (d.block + sc_off) * PER) & low5) << 5) + sc_byte));
+    };
+    const Rsrc xr = make_rsrc(x, batch * x_row);
+    auto load_x = [&](uint32_t s, u32x4 (&to)[4]) __attribute__((always_inline)) {
+        if (XL) {
+            const u32x4 *const from = s_x + min(s, v.segs - 1u) * 16u * batch + x_lds;
+#pragma unroll
+            for (uint32_t k = 0; k < 4u; ++k)
+                to[k] = from[k * 4u * batch];
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < 4u; ++k)
+                to[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                    xr, s * 128u + 32u * k < v.cols ? x_at + (s * 128u + 32u * k) * 2u : kQ4Outside, 0, 0));
+        }
+    };
+    bool begun = false;
+    Unit next_unit;   // the one whose loads are made next
+    auto prime = [&](uint32_t t, uint32_t next) __attribute__((always_inline)) {
+        const Unit d = unit_of(t, 0u);
+        next_unit = unit_of(units > 1u ? t : next, units > 1u ? 1u : 0u);
+        load_scales(d);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            load_codes(d, b);
+        if (!XL)
+            load_x(first, xs[0]);
+        begun = false;
+    };
+    auto prologue = [&]() __attribute__((always_inline)) {
+        if (XL) {
+            const uint32_t n = v.segs * 16u * batch;
+            for (uint32_t i = threadIdx.x; i < n; i += kQ4Threads) {
+                const uint32_t b = i % batch, k = i / batch * 8u;  // columns in order: [segment][step][4]
+                u32x4 z = {0u, 0u, 0u, 0u};
+                if (k < v.cols)
+                    z = *reinterpret_cast<const u32x4 *>(x + (uint64_t)b * x_row + k * 2u);
+                s_x[i] = z;
+            }
+        }
+    };
+    uint32_t turn = 0u;
+    auto body = [&](uint32_t t, uint32_t next, uint32_t after, uint32_t &) __attribute__((always_inline)) {
+        float total[R][4] = {};
+        if (XL && !begun)
+            load_x(first, xs[0]);
+        begun = true;
+        for (uint32_t u = 0; u < units; ++u) {
+            const bool end = u + 1u == units;
+            const Unit d = next_unit;
+            // the entries of the unit after the next
+            next_unit = end ? (units > 1u ? unit_of(next, 1u) : unit_of(after, 0u))
+                            : u + 2u < units ? unit_of(t, u + 2u) : unit_of(next, 0u);
+            // this unit's scales, in fp32
+            if (my_plane < (uint32_t)PLANES) {
+                f32x4 lo, hi;
+                q4_widen<DT>(sc, lo, hi);
+                if (ZEROS) {
+                    const float add = my_plane ? 16.0f : 0.0f;
+                    lo += add;
+                    hi += add;
+                }
+                s_sc[wave][lane * 2u] = lo;
+                s_sc[wave][lane * 2u + 1u] = hi;
+            }
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                u32x4 xb[4];
+#pragma unroll
+                for (uint32_t k = 0; k < 4u; ++k)
+                    xb[k] = xs[NS > 1 ? i % 2 : 0][k];
+                load_x(first + (i + 1 < NS ? u * NS + i + 1u : end ? 0u : (u + 1u) * NS), xs[NS > 1 ? (i + 1) % 2 : 0]);
+                constexpr int kSteps = 4 / PER;
+#pragma unroll
+                for (int p = 0; p < PER; ++p) {
+                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = p * kSteps; k < (p + 1) * kSteps; ++k)
+                        o = q4_mfma<DT>(off, xb[k], o);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const u32x4 ww = w[r][i];
+                        const uint32_t wk[4] = {ww.x, ww.y, ww.z, ww.w};
+                        f32x4 acc = ZEROS ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : o;
+#pragma unroll
+                        for (int k = p * kSteps; k < (p + 1) * kSteps; ++k)
+                            acc = q4_mfma<DT>(q4_codes<DT>(wk[k], one), xb[k], acc);
+                        const uint32_t at = ((r * NS + i) * 4u + grp) * PER + p;
+                        const f32x4 f = s_sc[wave][at];
+                        f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if (ZEROS)
+                            z = s_sc[wave][PLANE * 2u + at];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float dot = ZEROS ? __builtin_fmaf(z[j], o[j], acc[j]) : acc[j];
+                            total[r][j] = __builtin_fmaf(f[j], dot, total[r][j]);
+                            // (left to themselves the sums sink to the unit's end, past all loads)
+                            asm volatile("" : "+v"(total[r][j]));
+                        }
+                        if (p == PER - 1) {
+                            if (i == 0 && r == 0)
+                                load_scales(d);
+                            load_codes(d, r * NS + i);
+                        }
+                        if (p == PER - 1 || PER == 4)
+                            __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            s_red[turn % RB][wave][r][lane] = f32x4{total[r][0], total[r][1], total[r][2], total[r][3]};
+        __syncthreads();
+        // (with two buffers, one is written again only after the next tile's barrier)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (wave == (turn + r * (kQ4Waves / R)) % (uint32_t)kQ4Waves) {
+                f32x4 sum = s_red[turn % RB][0][r][lane];
+#pragma unroll
+                for (int i = 1; i < kQ4Waves; ++i)
+                    sum += s_red[turn % RB][i][r][lane];
+                if (col < batch) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 4u; ++j) {
+                        const uint32_t m = (t * R + r) * 16u + grp * 4u + j;
+                        if (m < v.rows)
+                            y[(uint64_t)col * v.rows + m] = sum[j];
+                    }
+                }
+            }
+        }
+        turn += 1u;
+        if (RB == 1)
+            __syncthreads();
+    };
+    single_tile_stream(g, n_tiles, prime, prologue, body);
+    if (bad)
+        raise_flag(g.err, bad);
 }
 
 // A tile is kPackBlocks blocks; a thread writes a lane's piece of 16 bytes from
@@ -174,14 +320,14 @@ __global__ __launch_bounds__(kQ4Threads) void k_gemv_q4(Q4View v, const uint8_t 
 constexpr int kPackThreads = 256;
 
 template <typename F>
-__device__ __forceinline__ void q4_store(const Q4View &v, uint64_t byte, uint32_t &err, F store)
+__device__ __forceinline__ void q4_store(const Q4View &v, const uint32_t *pt, uint64_t byte, uint32_t &err, F store)
 {
-    const uint32_t e = checked_page(v.pt, byte >> v.shift, v.pool_pages, err);
+    const uint32_t e = checked_page(pt, byte >> v.shift, v.pool_pages, err);
     if (e != kBadPage)
         store(const_cast<uint8_t *>(v.pool) + ((uint64_t)e << v.shift) + (byte & ((1ull << v.shift) - 1ull)));
 }
 
-__global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, uint32_t per, const uint8_t *__restrict__ codes,
+__global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, const uint32_t *__restrict__ pt, uint32_t per, const uint8_t *__restrict__ codes,
                                                           uint64_t stride, const uint16_t *__restrict__ scales,
                                                           const uint16_t *__restrict__ zeros, uint64_t n_blocks,
                                                           uint32_t n_tiles, Gate g)
@@ -207,7 +353,7 @@ __global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, uint32_t per
                 }
                 o[i] = w;
             }
-            q4_store(v, block * kQ4Block + lane * 16u, err, [&](uint8_t *p) { *reinterpret_cast<u32x4 *>(p) = o; });
+            q4_store(v, pt, block * kQ4Block + lane * 16u, err, [&](uint8_t *p) { *reinterpret_cast<u32x4 *>(p) = o; });
             const uint32_t row = lane / per, grp = lane % per;  // 16 * per scales
             if (row < 16u) {
                 const uint64_t mm = tile * 16u + row;
@@ -215,15 +361,20 @@ __global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, uint32_t per
                 const bool in = mm < v.rows && gg < n;
                 const uint64_t at = block * (per * 32u) + (((row / 4u) * per + grp) * 4u + row % 4u) * 2u;
                 const uint16_t s = in ? scales[mm * n + gg] : (uint16_t)0;
-                q4_store(v, v.scales + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = s; });
+                q4_store(v, pt, v.scales * 32ull + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = s; });
                 if (zeros) {
                     const uint16_t z = in ? zeros[mm * n + gg] : (uint16_t)0;
-                    q4_store(v, v.zeros + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = z; });
+                    q4_store(v, pt, v.zeros * 32ull + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = z; });
                 }
             }
         }
     };
     tile_loop<Claim::Ahead>(g, n_tiles, NoOp(), body);
+}
+
+static uint64_t q4_blocks(const sgdrc_q4 *q)
+{
+    return ((uint64_t)q->rows + 15u) / 16u * ((q->cols + 127u) / 128u);
 }
 
 static int check_q4(const sgdrc_q4 *q)
@@ -240,35 +391,106 @@ static int check_q4(const sgdrc_q4 *q)
         return set_error(SGDRC_EINVAL, "q: more than 65536 columns");
     if (q->zeros > 1 || q->reserved)
         return set_error(SGDRC_EINVAL, "q: zeros must be 0 or 1, reserved 0");
+    if (q4_blocks(q) >= (1ull << 26))
+        return set_error(SGDRC_EINVAL, "q: 2^26 blocks or more");
     return SGDRC_OK;
-}
-
-static uint64_t q4_blocks(const sgdrc_q4 *q)
-{
-    return ((uint64_t)q->rows + 15u) / 16u * ((q->cols + 127u) / 128u);
 }
 
 static uint64_t q4_scale_bytes(const sgdrc_q4 *q) { return q4_blocks(q) * (128u / q->group) * 32u; }
 
 static Q4View q4_view(const sgdrc_paged *w, const sgdrc_q4 *q, uint32_t page_shift)
 {
-    const uint64_t s = q4_blocks(q) * kQ4Block;
-    return {static_cast<const uint8_t *>(w->pool), w->pt, w->pool_pages, s, s + q4_scale_bytes(q), page_shift,
-            q->rows, q->cols, (q->cols + 127u) / 128u};
+    const uint32_t s = (uint32_t)(q4_blocks(q) * (kQ4Block / 32u));
+    return {static_cast<const uint8_t *>(w->pool), w->pool_pages, s, s + (uint32_t)(q4_scale_bytes(q) / 32u),
+            page_shift, q->rows, q->cols, (q->cols + 127u) / 128u};
 }
 
-typedef void (*Q4Kernel)(Q4View, const uint8_t *, uint32_t, float *, uint32_t, Gate);
+typedef void (*Q4Kernel)(Q4View, const uint32_t *, const uint8_t *, uint32_t, uint32_t, float *, uint32_t, Gate);
 
-template <int DT, int PER>
-static Q4Kernel q4_kernel(const sgdrc_q4 *q)
+// Which form of the kernel a call takes: the row blocks of a tile, and where x is.
+// None changes a result.
+//
+// More row blocks share a segment's x and offset and give a wavefront independent
+// chains; fewer spread a small matrix over the CUs.  x in LDS does not queue behind the
+// codes, but every workgroup stages it.  bf16, 2 MiB pages, rotated copies on MI355X, us:
+//                                     1, x in LDS   1, L2   2, LDS   4, L2
+//   4096 x 11008, batch 1                    10.7    11.5     13.6    19.6
+//   11008 x 4096, batch 1                    10.2    10.7     11.4    11.0
+//   11008 x 4096, batch 8                    13.4    13.7     14.3    11.2
+//   the same, groups of 32 with zero points  15.5    14.5     16.2    14.1
+//   and batch 4                              13.1    12.1     15.5    14.3
+//   16384 x 8192, batch 1                    20.2      -      17.9    19.3
+//   16384 x 8192, batch 4                    22.6      -      20.3    19.3
+//   32768 x 8192, batch 1                    29.4    37.9     28.7    31.7
+//   32768 x 8192, batch 16, groups of 64       -     69.6       -     37.3
+//   131072 x 8192, batch 1                  110        -      98.7    96.5
+//   8192 x 1024, batch 4                      8.8     9.1      7.0     6.5
+struct Q4Plan {
+    uint32_t blocks;  // of rows, a tile: 1, 2 or 4
+    bool x_lds;
+};
+
+constexpr uint64_t kQ4XLds = 24576;  // bytes of x in LDS at most
+
+static Q4Plan q4_plan(const sgdrc_q4 *q, uint32_t batch, uint32_t allowed)
 {
-    return q->zeros ? k_gemv_q4<DT, PER, true> : k_gemv_q4<DT, PER, false>;
+    const uint32_t segs = (q->cols + 127u) / 128u;
+    const uint64_t row_blocks = ((uint64_t)q->rows + 15u) / 16u, cus = std::max(allowed, 1u);
+    const bool fits = (uint64_t)segs * 256u * batch <= kQ4XLds;
+    if (segs <= (uint32_t)kQ4Waves && row_blocks >= 2u * cus)
+        return {4u, false};
+    if (row_blocks > 3u * cus) {
+        if (fits && batch <= 2u && row_blocks <= 8u * cus)
+            return {2u, true};
+        return {4u, false};
+    }
+    if (batch > 4u && 2u * row_blocks >= 5u * cus)
+        return {4u, false};
+    return {1u, fits};
+}
+
+template <int DT, int PER, bool ZEROS>
+static Q4Kernel q4_form(const Q4Plan &p)
+{
+    if (p.blocks == 4u)
+        return k_gemv_q4<DT, PER, ZEROS, 4, false>;
+    if (p.blocks == 2u)
+        return k_gemv_q4<DT, PER, ZEROS, 2, true>;
+    return p.x_lds ? k_gemv_q4<DT, PER, ZEROS, 1, true> : k_gemv_q4<DT, PER, ZEROS, 1, false>;
 }
 
 template <int DT>
-static Q4Kernel q4_kernel_group(const sgdrc_q4 *q)
+static Q4Kernel q4_kernel(const sgdrc_q4 *q, const Q4Plan &p)
 {
-    return q->group == 128 ? q4_kernel<DT, 1>(q) : q->group == 64 ? q4_kernel<DT, 2>(q) : q4_kernel<DT, 4>(q);
+    switch (128u / q->group) {
+    case 1: return q->zeros ? q4_form<DT, 1, true>(p) : q4_form<DT, 1, false>(p);
+    case 2: return q->zeros ? q4_form<DT, 2, true>(p) : q4_form<DT, 2, false>(p);
+    default: return q->zeros ? q4_form<DT, 4, true>(p) : q4_form<DT, 4, false>(p);
+    }
+}
+
+constexpr uint32_t kLdsBytes = 163840u;  // of a CU
+
+// Workgroups of a kernel that fit a CU with ``dynamic`` bytes of LDS each beside its own.
+static int q4_occupancy(Q4Kernel k, uint32_t dynamic)
+{
+    struct Fit {
+        int regs;
+        uint32_t lds;
+    };
+    static std::mutex mu;
+    static std::unordered_map<const void *, Fit> cache;
+    std::lock_guard<std::mutex> lock(mu);
+    auto it = cache.find((const void *)k);
+    if (it == cache.end()) {
+        hipFuncAttributes a{};
+        Fit f = {occupancy(k, kQ4Threads), kLdsBytes};
+        if (hipFuncGetAttributes(&a, (const void *)k) == hipSuccess)
+            f.lds = (uint32_t)a.sharedSizeBytes;
+        it = cache.emplace((const void *)k, f).first;
+    }
+    const uint32_t lds = it->second.lds + dynamic;
+    return std::min(it->second.regs, (int)(kLdsBytes / std::max(lds, 1u)));
 }
 
 }  // namespace sgdrc
@@ -303,8 +525,6 @@ int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q, c
     if (code_stride < q->cols || code_stride > (1ull << 40))
         return set_error(SGDRC_EINVAL, "code_stride %llu", (unsigned long long)code_stride);
     const uint64_t blocks = q4_blocks(q), tiles = (blocks + kPackThreads / 64 - 1) / (kPackThreads / 64);
-    if (blocks >= (1ull << 31))
-        return set_error(SGDRC_EINVAL, "2^31 blocks or more");
     Ctx *c = nullptr;
     if ((rc = check_ctx(ctx, &c)))
         return rc;
@@ -315,7 +535,7 @@ int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q, c
     static const int occ = occupancy(k_q4_pack, kPackThreads);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(k_q4_pack, dim3(gated_grid(c, occ, tiles, li)), dim3(kPackThreads), 0, s,
-                       q4_view(dst, q, page_shift), 128u / q->group, d_codes, code_stride,
+                       q4_view(dst, q, page_shift), dst->pt, 128u / q->group, d_codes, code_stride,
                        static_cast<const uint16_t *>(d_scales), static_cast<const uint16_t *>(d_zeros), blocks,
                        (uint32_t)tiles, g);
     SGDRC_HIP(hipGetLastError());
@@ -338,16 +558,22 @@ int colored_gemv_q4(sgdrc_ctx *ctx, const sgdrc_paged *w, const sgdrc_q4 *q, con
     Ctx *c = nullptr;
     if ((rc = check_ctx(ctx, &c)))
         return rc;
-    const uint64_t tiles = ((uint64_t)q->rows + 15u) / 16u;
+    const Q4Plan p = q4_plan(q, batch, (uint32_t)stream_allowed_cus(c, stream));
+    const uint32_t segs = (q->cols + 127u) / 128u;
+    const uint64_t tiles = (((uint64_t)q->rows + 15u) / 16u + p.blocks - 1u) / p.blocks;
     Gate g;
     LaunchInfo li;
-    if ((rc = make_gate(c, stream, tiles, kGemvGroupCus, &g, &li, false, true)))
+    if ((rc = make_gate(c, stream, tiles, kStreamGroupCus, &g, &li, false, true)))
         return rc;
-    const Q4Kernel k = q->dtype == SGDRC_BF16 ? q4_kernel_group<SGDRC_BF16>(q) : q4_kernel_group<SGDRC_F16>(q);
-    static const int occ = occupancy(k_gemv_q4<SGDRC_BF16, 4, true>, kQ4Threads);
+    const Q4Kernel k = q->dtype == SGDRC_BF16 ? q4_kernel<SGDRC_BF16>(q, p) : q4_kernel<SGDRC_F16>(q, p);
+    const uint32_t lds = p.x_lds ? segs * 256u * batch : 0u;
+    const int occ = q4_occupancy(k, lds);
+    if (occ < 1)
+        return set_error(SGDRC_EINVAL, "the kernel does not fit a CU (library fault)");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(k, dim3(gated_grid(c, occ, tiles, li)), dim3(kQ4Threads), 0, s, q4_view(w, q, page_shift),
-                       static_cast<const uint8_t *>(d_x), batch, d_y, (uint32_t)tiles, g);
+    hipLaunchKernelGGL(k, dim3(gated_grid(c, occ, tiles, li)), dim3(kQ4Threads), lds, s,
+                       q4_view(w, q, page_shift), w->pt, static_cast<const uint8_t *>(d_x), batch,
+                       (segs + kQ4Waves - 1u) / kQ4Waves, d_y, (uint32_t)tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);
 }

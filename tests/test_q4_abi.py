@@ -63,7 +63,8 @@ def test_bad_arguments(L):
         assert pack(L, **kw) == sg.EINVAL, kw
     for kw in (dict(x=None), dict(x=264), dict(y=None), dict(y=258), dict(batch=0), dict(batch=17), dict(shift=9)):
         assert gemv(L, **kw) == sg.EINVAL, kw
-    assert pack(L, q=q4(rows=(1 << 32) - 1, cols=1024)) == sg.EINVAL     # 2^31 blocks
+    assert pack(L, q=q4(rows=1 << 27, cols=1024), stride=1024) == sg.EINVAL     # 2^26 blocks
+    assert gemv(L, q=q4(rows=(1 << 32) - 1, cols=1024)) == sg.EINVAL
     n = ctypes.c_uint64()
     assert L.sgdrc_q4_bytes(r(q4()), None) == L.sgdrc_q4_bytes(None, r(n)) == sg.EINVAL
     assert "NULL" in sg.last_error()
