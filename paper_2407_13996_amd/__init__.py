@@ -587,8 +587,17 @@ def _written_rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
     return r
 
 
+_DTYPES = {}
+
+
 def _dtype_of(t) -> int:
-    return {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}.get(str(t.dtype), -1)
+    """F32, BF16 or F16 of a tensor, -1 for others (a type's name is asked for once: it
+    takes longer than the rest of a call's checks)."""
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        d = _DTYPES[t.dtype] = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}.get(str(t.dtype),
+                                                                                                     -1)
+    return d
 
 
 def colored_kv_map(ctx, block_tokens: int, ring, ring_pos, held, lens, new, table, ring_pos_out, held_out, lens_out,
