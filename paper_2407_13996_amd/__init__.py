@@ -546,11 +546,20 @@ def kv_cache(pool, pool_pages: int, page_shift: int, block_tokens: int, kv_heads
     return c
 
 
+_SIZES = {}
+
+
+def _size_of(t) -> int:
+    """Bytes of a tensor's whole numbers, 0 if they are none (asked for once a type)."""
+    _SIZES[t.dtype] = 0 if t.is_floating_point() else t.element_size()
+    return _SIZES[t.dtype]
+
+
 def _ints_of(t, name: str, size: int = 4):
     """Device address of a contiguous tensor of ``size``-byte whole numbers."""
     if t is None or not hasattr(t, "data_ptr"):
         return _addr(t)
-    if t.element_size() != size or t.is_floating_point() or not t.is_contiguous():
+    if _SIZES.get(t.dtype) != size and _size_of(t) != size or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of {8 * size}-bit whole numbers")
     return t.data_ptr()
 
@@ -567,23 +576,30 @@ def _blocks(table) -> KvBlocks:
 
 def _rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
     """Rows of heads of a [tokens, heads, dim] tensor, the last dimension without gaps."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or (t.stride(2) != 1 and t.numel()):
+    return _rows_of(t, name, heads, dim, dtype)[0]
+
+
+def _rows_of(t, name: str, heads: int, dim: int, dtype: int):
+    """(Rows, tokens) of such a tensor."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or (strides[2] != 1 and t.numel()):
         raise ValueError(f"{name} must be [tokens, {heads}, {dim}], the last dimension contiguous")
-    if (F32, BF16, F16)[dtype] != _dtype_of(t):
+    if _dtype_of(t) != dtype or dtype < 0:
         raise ValueError(f"{name} is not of the cache's dtype")
     # a stride that no second token or head uses says nothing
-    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if heads > 1 else 0)
+    n = shape[0]
+    return Rows(t.data_ptr(), strides[0] if n > 1 else 0, strides[1] if heads > 1 else 0), n
 
 
 def _written_rows(t, name: str, heads: int, dim: int, dtype: int) -> Rows:
     """The same for rows that are written: none of them may share memory."""
-    r = _rows(t, name, heads, dim, dtype)
-    spans = sorted((s, n) for s, n in ((t.stride(0), t.shape[0]), (t.stride(1), heads)) if n > 1)
-    end = dim
-    for stride, n in spans:
-        if stride < end:
-            raise ValueError(f"{name} has rows that overlap")
-        end += stride * (n - 1)
+    r, n = _rows_of(t, name, heads, dim, dtype)
+    step, n_step, wide, n_wide = r.head_stride, heads, r.token_stride, n
+    if n_step < 2 or (n_wide > 1 and wide < step):
+        step, n_step, wide, n_wide = wide, n_wide, step, n_step
+    # the closer ones apart by a row at least, the others by all of those
+    if (n_step > 1 and step < dim) or (n_wide > 1 and wide < (step * (n_step - 1) if n_step > 1 else 0) + dim):
+        raise ValueError(f"{name} has rows that overlap")
     return r
 
 
@@ -642,22 +658,29 @@ def colored_kv_append_rotated(ctx, cache: KvCache, layer: int, q, k, v, q_out, s
     first 2 * len(``freq``) dimensions turned by position * freq (fp32, radians;
     pairs of halves, or of neighbours if ``interleaved``).  q [tokens, heads, head_dim] goes to
     ``q_out`` (which may be q).  ``position`` (int32): below 0, a token is left out."""
-    n, heads = slots.numel(), q.shape[1]
-    if not (q.shape[0] == k.shape[0] == v.shape[0] == position.numel() == n and q_out.shape == q.shape):
+    heads, dim, dtype, kv = q.shape[1], cache.head_dim, cache.dtype, cache.kv_heads
+    rows_q, n = _rows_of(q, "q", heads, dim, dtype)
+    rows_k, n_k = _rows_of(k, "k", kv, dim, dtype)
+    rows_v, n_v = _rows_of(v, "v", kv, dim, dtype)
+    if not (n == n_k == n_v == slots.numel() == position.numel() and q_out.shape == q.shape):
         raise ValueError("q, k, v, q_out, slots and position must have as many tokens, q_out the heads of q")
-    norms = [t for t in (q_norm, k_norm) if t is not None]
-    for t in norms:
-        if not (_dtype_of(t) == _dtype_of(norms[0]) >= 0 and t.is_contiguous() and t.numel() == cache.head_dim):
-            raise ValueError("the norms' weights must be contiguous [head_dim], of one floating type")
-    if freq is not None and not (_dtype_of(freq) == F32 and freq.is_contiguous()):
-        raise ValueError("freq must be a contiguous fp32 tensor")
-    turn = Rotation(_addr(q_norm), _addr(k_norm), _addr(freq) if freq is not None and freq.numel() else None,
-                    _dtype_of(norms[0]) if norms else F32, 0 if freq is None else 2 * freq.numel(),
-                    int(bool(interleaved)), float(eps))
-    row = (cache.head_dim, cache.dtype)
-    _check(lib().colored_kv_append_rotated(_h(ctx), cache, int(layer), _rows(q, "q", heads, *row), heads,
-                                           _written_rows(q_out, "q_out", heads, *row),
-                                           _rows(k, "k", cache.kv_heads, *row), _rows(v, "v", cache.kv_heads, *row),
+    norm = F32
+    for t in (q_norm, k_norm):
+        if t is not None:
+            norm = _dtype_of(t)
+            if norm < 0 or t.numel() != dim or not t.is_contiguous():
+                raise ValueError("the norms' weights must be contiguous [head_dim], of one floating type")
+    if q_norm is not None and k_norm is not None and q_norm.dtype != k_norm.dtype:
+        raise ValueError("the norms' weights must be contiguous [head_dim], of one floating type")
+    half = 0
+    if freq is not None:
+        half = freq.numel()
+        if not (_dtype_of(freq) == F32 and freq.is_contiguous()):
+            raise ValueError("freq must be a contiguous fp32 tensor")
+    turn = Rotation(None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(),
+                    freq.data_ptr() if half else None, norm, 2 * half, 1 if interleaved else 0, eps)
+    _check(lib().colored_kv_append_rotated(_h(ctx), cache, layer, rows_q, heads,
+                                           _written_rows(q_out, "q_out", heads, dim, dtype), rows_k, rows_v,
                                            _ints_of(slots, "slots", 8), _ints_of(position, "position"), n, turn,
                                            _stream(stream)))
 
@@ -671,32 +694,31 @@ def colored_draft_verify(ctx, target, tokens, parents, uniform, q_start, path, a
     the request's own count) and ``uniform`` (fp32, [0, 1)): an entry a node, the root's random
     number is the next token's.  ``lens``, ``totals``: as for the attention; a
     request that was not served accepts nothing.  path, accepted and lens, totals go on to colored_kv_commit."""
-    n, requests = tokens.numel(), q_start.numel() - 1
-    if not (target.dim() == 2 and target.shape[0] == n == parents.numel() == uniform.numel() and path.dim() == 2
-            and path.shape[0] == requests == accepted.numel() == next.numel()):
+    n, requests, shape, most = tokens.numel(), q_start.numel() - 1, target.shape, path.shape
+    if not (len(shape) == 2 and shape[0] == n == parents.numel() == uniform.numel() and len(most) == 2
+            and most[0] == requests == accepted.numel() == next.numel()):
         raise ValueError("the arrays' lengths do not fit the requests and their nodes")
-    if any(t is not None and t.numel() != requests for t in (lens, totals)):
+    if (lens is not None and lens.numel() != requests) or (totals is not None and totals.numel() != requests):
         raise ValueError("lens and totals must have an entry a request")
-    if draft is not None and not (draft.shape == target.shape and draft.dtype == target.dtype):
+    dtype, vocab = _dtype_of(target), shape[1]
+    if dtype < 0:
+        raise ValueError("probabilities must be fp32, bf16 or fp16")
+    if draft is not None and not (draft.shape == shape and draft.dtype == target.dtype):
         raise ValueError("draft must be as target")
-    for t in (target, draft):
-        if t is not None and t.numel() and t.stride(1) != 1 and t.shape[1] > 1:
-            raise ValueError("rows of probabilities must have no gaps inside")
+    strides = [vocab, vocab]
+    for i, t in enumerate((target, draft)):
+        if t is not None and n:
+            row, step = t.stride()
+            if step != 1 and vocab > 1:
+                raise ValueError("rows of probabilities must have no gaps inside")
+            strides[i] = row if n > 1 else vocab
     if not (_dtype_of(uniform) == F32 and uniform.is_contiguous()):
         raise ValueError("uniform must be a contiguous fp32 tensor")
-    if _dtype_of(target) < 0:
-        raise ValueError("probabilities must be fp32, bf16 or fp16")
-    vocab = target.shape[1]
-
-    def stride(t):
-        return vocab if t is None or n < 2 else t.stride(0)
-
-    _check(lib().colored_draft_verify(_h(ctx), _dtype_of(target), vocab, _addr(target), stride(target), _addr(draft),
-                                      stride(draft), _ints_of(tokens, "tokens"), _ints_of(parents, "parents"),
-                                      _addr(uniform), n, _ints_of(q_start, "q_start"), requests, int(max_nodes),
-                                      _ints_of(lens, "lens"), _ints_of(totals, "totals"), _ints_of(path, "path"),
-                                      path.shape[1], _ints_of(accepted, "accepted"), _ints_of(next, "next"),
-                                      _stream(stream)))
+    _check(lib().colored_draft_verify(_h(ctx), dtype, vocab, target.data_ptr(), strides[0], _addr(draft), strides[1],
+                                      _ints_of(tokens, "tokens"), _ints_of(parents, "parents"), uniform.data_ptr(), n,
+                                      _ints_of(q_start, "q_start"), requests, max_nodes, _ints_of(lens, "lens"),
+                                      _ints_of(totals, "totals"), _ints_of(path, "path"), most[1],
+                                      _ints_of(accepted, "accepted"), _ints_of(next, "next"), _stream(stream)))
 
 
 def colored_kv_commit(ctx, cache: KvCache, table, lens, path, accepted, lens_out, stream=None, totals=None) -> None:

@@ -46,7 +46,8 @@ def test_bad_arguments():
     assert sg.lib().colored_kv_append_rotated(None, r(cache()), 0, r(rows()), 8, r(rows()), r(rows()), r(rows()), 256,
                                               256, 1, None, None) == sg.EINVAL
     for kw in (dict(layer=1), dict(heads=0), dict(heads=12), dict(heads=1032), dict(slots=None), dict(slots=260),
-               dict(position=None), dict(position=258), dict(n=1 << 31), dict(n=(1 << 31) - 1, heads=1024)):
+               dict(position=None), dict(position=258), dict(n=1 << 31),
+               dict(n=(1 << 31) - 1, heads=256, c=cache(kv_heads=256, head_dim=64, block_tokens=16, page_shift=20))):
         assert call(**kw) == sg.EINVAL, kw
     for bad in (dict(ptr=0), dict(ptr=264), dict(token_stride=1020), dict(head_stride=4), dict(token_stride=(1 << 30) + 8)):
         for name in ("q", "out", "k", "v"):
