@@ -34,7 +34,8 @@
  *    on, wherever it is replayed: order replays with each other and with that
  *    stream's launches, as launches on one stream are.  (Launches under the
  *    static schedule, see set_cu_mask, use the queue for a classify's
- *    histogram and the time log only; others may overlap.)
+ *    histogram, a draft verification's sums and the time log only; others may
+ *    overlap.)
  *  - Page tables are arrays of uint32 pool-page indices.  Logical byte b of
  *    a paged tensor lives at pool + pt[b >> page_shift] * 2^page_shift +
  *    (b & (2^page_shift - 1)).  Kernels check every page-table entry

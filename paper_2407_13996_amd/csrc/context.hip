@@ -451,6 +451,7 @@ static void free_ctx(Ctx *c)
     if (c->d_lut) (void)hipFree(c->d_lut);
     if (c->d_queues) (void)hipFree(c->d_queues);
     if (c->d_hist_acc) (void)hipFree(c->d_hist_acc);
+    if (c->d_verify) (void)hipFree(c->d_verify);
     if (c->d_err) (void)hipFree(c->d_err);
     if (c->d_scratch) (void)hipFree(c->d_scratch);
     if (c->h_pinned) (void)hipHostFree(c->h_pinned);
@@ -508,6 +509,8 @@ int sgdrc_init(int device, sgdrc_ctx **out)
                   (size_t)kMaxStreams * kHistAccCopies * kHistBins * sizeof(uint64_t)));
     TRY(hipMemset(c->d_hist_acc, 0,
                   (size_t)kMaxStreams * kHistAccCopies * kHistBins * sizeof(uint64_t)));
+    TRY(hipMalloc(&c->d_verify, (size_t)kMaxStreams * (kVerifySums + kVerifyShared) * sizeof(uint64_t)));
+    TRY(hipMemset(c->d_verify, 0, (size_t)kMaxStreams * (kVerifySums + kVerifyShared) * sizeof(uint64_t)));
     TRY(hipMalloc(&c->d_err, sizeof(uint32_t)));
     TRY(hipMemset(c->d_err, 0, sizeof(uint32_t)));
     TRY(hipHostMalloc(&c->h_pinned, 8 * sizeof(uint64_t), hipHostMallocDefault));

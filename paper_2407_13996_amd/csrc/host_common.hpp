@@ -24,6 +24,11 @@ constexpr int kHistBins = 256;
 // workgroup adds its counts to the copy of its XCD, so that the workgroups'
 // device-scope atomics spread over eight addresses per bin.
 constexpr int kHistAccCopies = 8;
+// Draft verifications of few requests share a row's sum between workgroups: the
+// sums of a stream (64-bit words) and the requests at most, a word each for who has
+// arrived.
+constexpr uint32_t kVerifySums = 65536;
+constexpr uint32_t kVerifyShared = 128;
 // CUs served by one work queue.  Long streaming kernels use one queue for
 // the whole device (0): tiles are then taken in address order by all CUs
 // together, which measured faster on MI355X than splitting the address range
@@ -98,6 +103,7 @@ struct Ctx {
     uint32_t *d_lut = nullptr;           // kLutSize entries: logical CU | group << 16
     QueueSlot *d_queues = nullptr;       // kMaxStreams
     uint64_t *d_hist_acc = nullptr;      // kMaxStreams x kHistAccCopies x kHistBins
+    uint64_t *d_verify = nullptr;        // kMaxStreams x (kVerifySums + kVerifyShared), zero at rest but for the sums
     uint32_t *d_err = nullptr;           // one word
 
     void *d_scratch = nullptr;           // page-table build scratch
