@@ -315,57 +315,93 @@ __global__ __launch_bounds__(kQ4Threads) __attribute__((amdgpu_waves_per_eu(4)))
         raise_flag(g.err, bad);
 }
 
-// A tile is kPackBlocks blocks; a thread writes a lane's piece of 16 bytes from
-// four runs of eight codes, and the threads past the pieces take the scales.
+// The packed layout is the codes' alone, so the kernel is a copy: 1 byte read and
+// half a byte written a weight.  A wavefront takes kPackBlocks blocks in a row, whose
+// loads go out together: eight lanes read the 128 codes of a row, 16 each, and have
+// by them one word of two pieces, so that both the reads and the stores run over
+// whole cache lines; the block's scales go through its first lanes.  The codes are
+// read once and stay out of the L2's way (nontemporal).  11008 x 4096: 16.3 us, 4.1 TB/s
+// (byte by byte 20.3; one block 20.4, four 19.4; ordinary loads 18.2).
 constexpr int kPackThreads = 256;
+constexpr uint32_t kPackBlocks = 2;
 
-template <typename F>
-__device__ __forceinline__ void q4_store(const Q4View &v, const uint32_t *pt, uint64_t byte, uint32_t &err, F store)
+struct __attribute__((packed, aligned(1))) Codes16 {
+    u32x4 v;
+};
+
+// The word of 8 codes: column e at bit 4 (e / 2 + 4 (e % 2)).
+__device__ __forceinline__ uint32_t q4_word(uint32_t lo, uint32_t hi)
 {
-    const uint32_t e = checked_page(pt, byte >> v.shift, v.pool_pages, err);
-    if (e != kBadPage)
-        store(const_cast<uint8_t *>(v.pool) + ((uint64_t)e << v.shift) + (byte & ((1ull << v.shift) - 1ull)));
+    auto two = [](uint32_t x) {
+        x &= 0x000F000Fu;
+        return (x | x >> 12) & 0xFFu;
+    };
+    return two(lo) | two(hi) << 8 | two(lo >> 8) << 16 | two(hi >> 8) << 24;
 }
 
-__global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, const uint32_t *__restrict__ pt, uint32_t per, const uint8_t *__restrict__ codes,
-                                                          uint64_t stride, const uint16_t *__restrict__ scales,
-                                                          const uint16_t *__restrict__ zeros, uint64_t n_blocks,
+// Where a byte of the matrix lies; nullptr and the flag if its page is none.
+__device__ __forceinline__ uint8_t *q4_place(const Q4View &v, const uint32_t *pt, uint64_t byte, uint32_t &err)
+{
+    const uint32_t e = checked_page(pt, byte >> v.shift, v.pool_pages, err);
+    return e == kBadPage ? nullptr
+                         : const_cast<uint8_t *>(v.pool) + ((uint64_t)e << v.shift) + (byte & ((1ull << v.shift) - 1ull));
+}
+
+__global__ __launch_bounds__(kPackThreads) void k_q4_pack(Q4View v, const uint32_t *__restrict__ pt, uint32_t per,
+                                                          const uint8_t *__restrict__ codes, uint64_t stride,
+                                                          const uint16_t *__restrict__ scales,
+                                                          const uint16_t *__restrict__ zeros, uint32_t n_blocks,
                                                           uint32_t n_tiles, Gate g)
 {
-    constexpr uint32_t kBlocks = kPackThreads / 64;
+    constexpr uint32_t kWaves = kPackThreads / 64;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t code_row = lane / 8u, eighth = lane % 8u;  // and the row 8 further
+    const uint32_t row = lane / per, grp = lane % per;  // of the block's 16 per scales, one a lane
+    const uint32_t n_groups = v.cols * per / 128u;
+    const uint32_t at = (((row / 4u) * per + grp) * 4u + row % 4u) * 2u;
     auto body = [&](uint32_t t, uint32_t, uint32_t &err, auto &&) {
-        const uint64_t block = (uint64_t)t * kBlocks + (threadIdx.x >> 6);
-        const uint32_t lane = threadIdx.x & 63u;
-        if (block < n_blocks) {
-            const uint64_t tile = block / v.segs;
-            const uint32_t seg = (uint32_t)(block % v.segs);
-            const uint64_t m = tile * 16u + (lane & 15u);
-            u32x4 o;
+        const uint32_t first = (t * kWaves + wave) * kPackBlocks;
+        u32x4 c[kPackBlocks][2];
+        uint16_t s[kPackBlocks], z[kPackBlocks];
 #pragma unroll
-            for (uint32_t i = 0; i < 4u; ++i) {
-                const uint32_t k = seg * 128u + i * 32u + (lane >> 4) * 8u;
-                uint32_t w = 0u;
-                if (m < v.rows && k < v.cols) {
-                    const uint8_t *const c = codes + m * stride + k;
+        for (uint32_t b = 0; b < kPackBlocks; ++b) {
+            const uint32_t block = first + b, tile = block / v.segs, seg = block % v.segs;
+            const uint32_t k = seg * 128u + eighth * 16u, gg = seg * per + grp;
+            const uint64_t m = tile * 16ull + code_row, mm = tile * 16ull + row;
 #pragma unroll
-                    for (uint32_t e = 0; e < 8u; ++e)
-                        w |= (uint32_t)(c[e] & 15u) << (4u * (e / 2u + 4u * (e % 2u)));
-                }
-                o[i] = w;
+            for (uint32_t h = 0; h < 2u; ++h) {
+                c[b][h] = u32x4{0u, 0u, 0u, 0u};
+                if (m + 8u * h < v.rows && k < v.cols)
+                    c[b][h] = __builtin_nontemporal_load(
+                        &reinterpret_cast<const Codes16 *>(codes + (m + 8u * h) * stride + k)->v);
             }
-            q4_store(v, pt, block * kQ4Block + lane * 16u, err, [&](uint8_t *p) { *reinterpret_cast<u32x4 *>(p) = o; });
-            const uint32_t row = lane / per, grp = lane % per;  // 16 * per scales
-            if (row < 16u) {
-                const uint64_t mm = tile * 16u + row;
-                const uint32_t gg = seg * per + grp, n = v.cols * per / 128u;
-                const bool in = mm < v.rows && gg < n;
-                const uint64_t at = block * (per * 32u) + (((row / 4u) * per + grp) * 4u + row % 4u) * 2u;
-                const uint16_t s = in ? scales[mm * n + gg] : (uint16_t)0;
-                q4_store(v, pt, v.scales * 32ull + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = s; });
-                if (zeros) {
-                    const uint16_t z = in ? zeros[mm * n + gg] : (uint16_t)0;
-                    q4_store(v, pt, v.zeros * 32ull + at, err, [&](uint8_t *p) { *reinterpret_cast<uint16_t *>(p) = z; });
+            s[b] = z[b] = 0u;
+            if (row < 16u && mm < v.rows && gg < n_groups) {
+                s[b] = scales[mm * n_groups + gg];
+                if (zeros)
+                    z[b] = zeros[mm * n_groups + gg];
+            }
+        }
+#pragma unroll
+        for (uint32_t b = 0; b < kPackBlocks; ++b) {
+            const uint32_t block = first + b;
+            if (block >= n_blocks)
+                break;
+            if (uint8_t *const p = q4_place(v, pt, (uint64_t)block * kQ4Block, err)) {
+                const uint32_t piece = eighth % 2u * 2u;
+                uint32_t *const words = reinterpret_cast<uint32_t *>(p) + (piece * 16u + code_row) * 4u + eighth / 2u;
+#pragma unroll
+                for (uint32_t h = 0; h < 2u; ++h) {
+                    words[h * 32u] = q4_word(c[b][h].x, c[b][h].y);
+                    words[h * 32u + 64u] = q4_word(c[b][h].z, c[b][h].w);
                 }
+            }
+            if (row < 16u) {
+                if (uint8_t *const p = q4_place(v, pt, v.scales * 32ull + (uint64_t)block * (per * 32u) + at, err))
+                    *reinterpret_cast<uint16_t *>(p) = s[b];
+                if (zeros)
+                    if (uint8_t *const p = q4_place(v, pt, v.zeros * 32ull + (uint64_t)block * (per * 32u) + at, err))
+                        *reinterpret_cast<uint16_t *>(p) = z[b];
             }
         }
     };
@@ -524,7 +560,8 @@ int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q, c
         return set_error(SGDRC_EINVAL, "scales and zero points must be 2-byte aligned");
     if (code_stride < q->cols || code_stride > (1ull << 40))
         return set_error(SGDRC_EINVAL, "code_stride %llu", (unsigned long long)code_stride);
-    const uint64_t blocks = q4_blocks(q), tiles = (blocks + kPackThreads / 64 - 1) / (kPackThreads / 64);
+    constexpr uint64_t kTile = kPackThreads / 64 * kPackBlocks;
+    const uint64_t blocks = q4_blocks(q), tiles = (blocks + kTile - 1) / kTile;
     Ctx *c = nullptr;
     if ((rc = check_ctx(ctx, &c)))
         return rc;
@@ -536,7 +573,7 @@ int colored_q4_pack(sgdrc_ctx *ctx, const sgdrc_paged *dst, const sgdrc_q4 *q, c
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(k_q4_pack, dim3(gated_grid(c, occ, tiles, li)), dim3(kPackThreads), 0, s,
                        q4_view(dst, q, page_shift), dst->pt, 128u / q->group, d_codes, code_stride,
-                       static_cast<const uint16_t *>(d_scales), static_cast<const uint16_t *>(d_zeros), blocks,
+                       static_cast<const uint16_t *>(d_scales), static_cast<const uint16_t *>(d_zeros), (uint32_t)blocks,
                        (uint32_t)tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);

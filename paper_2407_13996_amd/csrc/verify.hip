@@ -475,8 +475,8 @@ static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void
     if (rc)
         return rc;
     // Workgroups of a request: one a CU over all requests, each wavefront with a
-    // chunk, sums that fit the stream's place for them.  (64 chains of 8 nodes over 32768
-    // float values: 22 us, two a CU 31, without parts 37.  A chain over 131072: 13 and 30.)
+    // chunk, sums that fit the stream's place for them.  (Chains of 8 nodes over 131072
+    // float values, 64 of them: 22 us, two workgroups a CU 31, without parts 37.  One: 13 and 30.)
     a.parts = 1u;
     if (n_requests <= kVerifyShared && (uint64_t)n_requests * chunks <= kVerifySums)
         a.parts = std::max(1u, std::min({16u, (uint32_t)stream_allowed_cus(c, stream) / n_requests,
