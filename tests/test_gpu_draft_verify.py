@@ -261,3 +261,50 @@ def test_the_tokens_are_distributed_as_the_targets(ctx):
     total = 64 * n
     sigma = torch.sqrt(total * p.double() * (1 - p.double()))
     assert bool(((seen - total * p.double()).abs() <= 5 * sigma).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_shared_by_workgroups(ctx, dtype):
+    """Few requests over long rows, on CU masks that give each from sixteen workgroups to one, a graph
+    of two calls in a row with other inputs every replay, and launches between the replays."""
+    counts, vocab = [5, 0, 9], 270001
+    arrays = [case(counts, vocab, kind, dtype, 30 + i) for i, kind in enumerate(("chain", "tree", "star"))]
+    s = torch.cuda.Stream()
+    for cus in (None, range(64), range(12), [40, 41, 7], [17]):
+        sg.set_cu_mask(ctx, s, cus)
+        for args in arrays:
+            target, guess, *rest = args
+            t, d = target.to(DEV), guess.to(DEV)
+            s.wait_stream(torch.cuda.current_stream())
+            for draft, host in ((d, guess), (None, None)):
+                with torch.cuda.stream(s):
+                    got = call(ctx, t, draft, *rest)
+                s.synchronize()
+                compare(ctx, got, target, host, *rest)
+    sg.set_cu_mask(ctx, s, None)
+    bufs = [x.to(DEV) for x in arrays[0]]
+    outs = [[torch.zeros(3, 16, dtype=torch.int32, device=DEV)] +
+            [torch.zeros(3, dtype=torch.int32, device=DEV) for _ in range(2)] for _ in range(2)]
+
+    def go(out, drawn):
+        t, d, k, p, u, q = bufs
+        sg.colored_draft_verify(ctx, t, k, p, u, q, *out, draft=d if drawn else None)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        go(outs[0], True)
+        go(outs[1], False)
+    for args in arrays + arrays[:1]:
+        for b, x in zip(bufs, args):
+            b.copy_(x)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        compare(ctx, outs[0], *args, path_stride=16)
+        compare(ctx, outs[1], args[0], None, *args[2:], path_stride=16)
+        with torch.cuda.stream(s):
+            go(outs[0], False)
+        s.synchronize()
+        compare(ctx, outs[0], args[0], None, *args[2:], path_stride=16)
+    sg.stream_release(ctx, s)

@@ -227,3 +227,42 @@ def test_captured_and_replayed(ctx):
         torch.cuda.synchronize()
         assert torch.equal(again, y)
     sg.stream_release(ctx, s)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [sg.BF16, sg.F16])
+def test_same_bits_in_every_form(ctx, dtype, group, zeros):
+    """Fewer CUs have tiles of more rows, and small batches x in LDS: the number of
+    row blocks a CU has passes every bound of that choice, on whole XCDs and on parts."""
+    s = torch.cuda.Stream()
+    for rows, cols, batches in ((999, 1152, (1, 2, 3, 16)), (3300, 1152, (1, 6)), (2500, 256, (1, 16))):
+        m = Matrix(rows, cols, group, dtype, zeros, 13, seed=rows + group, negative=True).upload(ctx)
+        for batch in batches:
+            x = inputs(m, batch, seed=batch)
+            d_x, ys = x.to(DEV), []
+            for cus in (None, range(64), range(32), range(16), range(3, 7), [200]):
+                sg.set_cu_mask(ctx, s, cus)
+                ys.append(torch.full((batch, rows), -1.0, device=DEV))
+                s.wait_stream(torch.cuda.current_stream())
+                sg.colored_gemv_q4(ctx, m.w, m.q, d_x, batch, ys[-1], m.shift, stream=s)
+            s.synchronize()
+            check(m, x, ys[0])
+            assert all(torch.equal(y, ys[0]) for y in ys[1:])
+    sg.stream_release(ctx, s)
+    assert ctx.device_error() == 0
+
+
+def test_pack_on_any_cus(ctx):
+    m = Matrix(1003, 1056, 32, sg.F16, True, 12, seed=9).upload(ctx)
+    want = m.expect()
+    codes, scales, zeros = torch.from_numpy(m.codes).to(DEV), m.scales.to(DEV), m.zeros.to(DEV)
+    s = torch.cuda.Stream()
+    for cus in (None, range(64), range(5, 40), [17]):
+        sg.set_cu_mask(ctx, s, cus)
+        m.pool.copy_(m.before)
+        s.wait_stream(torch.cuda.current_stream())
+        sg.colored_q4_pack(ctx, m.w, m.q, codes, scales, zeros, m.shift, stream=s)
+        s.synchronize()
+        assert np.array_equal(m.pool.cpu().numpy(), want)
+    sg.stream_release(ctx, s)
