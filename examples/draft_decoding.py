@@ -85,6 +85,20 @@ def norm(x):
     return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-5)
 
 
+def masks_and_depths(trees):
+    """The nodes that each node of the trees sees (its ancestors and itself), as
+    words of bits, and how far below the root it is."""
+    words, depth = [], []
+    for _, parents in trees:
+        rows = []
+        for i, p in enumerate(parents):
+            rows.append((rows[p] if p >= 0 else 0) | 1 << i)
+            depth.append(bin(rows[-1]).count("1") - 1)
+        words += [[(r >> 64 * k) & (1 << 64) - 1 for k in range(MOST // 64)] for r in rows]
+    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in words], dtype=torch.int64,
+                        device=DEV), depth
+
+
 class Server:
     """The requests' state: the cache, its block tables and the free pages."""
 
@@ -121,15 +135,7 @@ class Server:
         counts = [len(t) for t, _ in trees]
         n = sum(counts)
         tokens = torch.tensor([t for tree, _ in trees for t in tree], device=DEV)
-        words, depth = [], []
-        for tree, parents in trees:
-            rows = []
-            for i, p in enumerate(parents):
-                rows.append((rows[p] if p >= 0 else 0) | 1 << i)
-                depth.append(bin(rows[-1]).count("1") - 1)
-            words += [[(r >> 64 * k) & (1 << 64) - 1 for k in range(MOST // 64)] for r in rows]
-        mask = torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in words], dtype=torch.int64,
-                            device=DEV)
+        mask, depth = masks_and_depths(trees)
         self.totals, q_start, slots = self.map(new, n)
         at = self.lens.repeat_interleave(torch.tensor(counts, device=DEV)).long() + torch.tensor(depth, device=DEV)
         x = self.w.embed[tokens].float() + self.w.place[at].float()
