@@ -125,7 +125,8 @@ __global__ __launch_bounds__(kQ4Threads) __attribute__((amdgpu_waves_per_eu(4)))
     const uint32_t my_code = lane & 3u, my_plane = lane / PLANE, my_block = lane % PLANE / PIECES;
     const uint32_t code_row = my_code / NS, code_seg = my_code % NS, sc_row = my_block / NS, sc_seg = my_block % NS;
     const uint32_t code_off = code_row * v.segs + code_seg, sc_off = sc_row * v.segs + sc_seg;
-    const uint32_t sc_base = my_plane ? v.zeros : v.scales, sc_byte = lane % PIECES * 16u;
+    // (lanes past the planes look up the last plane's entries: there are none behind the tensor's)
+    const uint32_t sc_base = ZEROS && my_plane ? v.zeros : v.scales, sc_byte = lane % PIECES * 16u;
     const uint32_t low10 = (1u << (v.shift - 10u)) - 1u, low5 = (1u << (v.shift - 5u)) - 1u;
 
     u32x4 w[R][NS];   // a unit's codes
