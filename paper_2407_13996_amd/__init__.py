@@ -533,6 +533,9 @@ def colored_q4_pack(ctx, dst: Paged, q: Q4, codes, scales, zeros=None, page_shif
 def colored_gemv_q4(ctx, w: Paged, q: Q4, x, batch: int, y, page_shift: int, stream=None) -> None:
     """y[b] = W x[b] for ``batch`` rows (1..16) of x (contiguous [batch, cols] of the
     matrix's dtype), y fp32 [batch, rows]."""
+    for t, name, dtype, width in ((x, "x", q.dtype, q.cols), (y, "y", F32, q.rows)):
+        if hasattr(t, "data_ptr") and (_dtype_of(t) != dtype or t.numel() < batch * width or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [{batch}, {width}], x of the matrix's dtype, y fp32")
     _check(lib().colored_gemv_q4(_h(ctx), w, q, _addr(x), int(batch), _addr(y), int(page_shift), _stream(stream)))
 
 

@@ -101,3 +101,16 @@ def test_the_layout_by_hand():
     assert out.nonzero()[0].tolist() == [3 * 1024 + (3 * 16 + 1) * 16 + 2 * 4 + 3, 4 * 1024 + 3 * 64 + 10,
                                          4 * 1024 + 3 * 64 + 11]
     assert out[3 * 1024 + 49 * 16 + 11] == 11
+
+
+def test_bindings_check_products():
+    q = sg.q4(4, 64, 32, sg.F16)
+    ok = dict(x=torch.zeros(2, 64, dtype=torch.float16), y=torch.zeros(2, 4))
+    for kw in (dict(x=torch.zeros(2, 64, dtype=torch.bfloat16)), dict(x=torch.zeros(1, 64, dtype=torch.float16)),
+               dict(x=torch.zeros(2, 128, dtype=torch.float16)[:, ::2]), dict(y=torch.zeros(2, 3)),
+               dict(y=torch.zeros(2, 4, dtype=torch.float16)), dict(y=torch.zeros(4, 2).t())):
+        with pytest.raises(ValueError):
+            sg.colored_gemv_q4(None, paged(), q, batch=2, page_shift=12, stream=0, **{**ok, **kw})
+    with pytest.raises(sg.SgdrcError) as e:
+        sg.colored_gemv_q4(None, paged(), q, batch=2, page_shift=12, stream=0, **ok)
+    assert e.value.code == sg.ENODEV
