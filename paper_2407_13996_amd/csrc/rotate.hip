@@ -196,7 +196,8 @@ __device__ __forceinline__ void turn_angle(int32_t position, float freq, float &
 // heads, of which U are on their way at a time, loaded together and then stored, so
 // that no load queues behind a store.  Values: as in k_kv_append.
 //
-// 16384 tokens of 32 + 8 + 8 heads of 128, 403 MB: 91 us on MI355X; U = 2 reloaded one by
+// 16384 tokens of 32 + 8 + 8 heads of 128, 403 MB: 91 us on MI355X (4.5 TB/s), without norms and
+// rotation too: the movement bounds it, in pieces of 128 bytes; U = 2 reloaded one by
 // one, four workgroups a CU, 104; U = 8, two workgroups, 102; U = 4, four workgroups, with
 // spilled registers, 110; a token's heads side by side, its angles by way of LDS, 114.
 template <int DT, int D, int TOKENS>

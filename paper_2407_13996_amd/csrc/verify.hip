@@ -120,6 +120,9 @@ __device__ __forceinline__ double wave_scan(double v, uint32_t lane)
 // as far as the first sum, share its chunks, and the last to have its part
 // goes on alone (a chain needs no other sum).  N: elements of a load (1 for a vocabulary
 // below a vector's).
+// Bound by the chain of its trips to memory (a chain of 5 over 32000: 12 us with the launch; 32 trees of up to
+// 48 certain choices over 50257: 26, a row's sum by one workgroup at each node that rejects),
+// with many long rows by the pass over them (64 chains of 8 over 131072, 67 MB: 22).
 template <int DT, uint32_t N>
 __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_draft_verify(
     VerifyArgs a, uint32_t n_tiles, Gate g)
