@@ -447,21 +447,24 @@ typedef void (*Q4Kernel)(Q4View, const uint32_t *, const uint8_t *, uint32_t, ui
 // Which form of the kernel a call takes: the row blocks of a tile, and where x is.
 // None changes a result.
 //
-// More row blocks share a segment's x and offset and give a wavefront independent
-// chains; fewer spread a small matrix over the CUs.  x in LDS does not queue behind the
-// codes, but every workgroup stages it.  bf16, 2 MiB pages, rotated copies on MI355X, us:
-//                                     1, x in LDS   1, L2   2, LDS   4, L2
-//   4096 x 11008, batch 1                    10.7    11.5     13.6    19.6
-//   11008 x 4096, batch 1                    10.2    10.7     11.4    11.0
-//   11008 x 4096, batch 8                    13.4    13.7     14.3    11.2
-//   the same, groups of 32 with zero points  15.5    14.5     16.2    14.1
-//   and batch 4                              13.1    12.1     15.5    14.3
-//   16384 x 8192, batch 1                    20.2      -      17.9    19.3
-//   16384 x 8192, batch 4                    22.6      -      20.3    19.3
-//   32768 x 8192, batch 1                    29.4    37.9     28.7    31.7
-//   32768 x 8192, batch 16, groups of 64       -     69.6       -     37.3
-//   131072 x 8192, batch 1                  110        -      98.7    96.5
-//   8192 x 1024, batch 4                      8.8     9.1      7.0     6.5
+// A wavefront with u segments goes through a tile in ceil(u / 4), ceil(u / 2) or u
+// units for 1, 2 or 4 row blocks, and a CU has ceil(tiles / CUs) tiles one after the
+// other or side by side.  A unit with one row block loads x for four segments, with
+// four blocks for one, which all blocks share; what it costs grows with the rows of x that
+// come out of LDS or the L2, while four blocks cost their codes, and more with zero points.  The form with the
+// least cost, in the weights below, is the best of the three in time but for 0.2 to 1.2 % on average
+// (at worst 19) over 1100 measured calls: all groups, with and without zero points, 2048 to 65536 rows,
+// 1024 to 11008 columns, batches 1 to 16, rotated copies.  bf16, 2 MiB pages, groups of 64, us:
+//                                                 1    2, x in LDS    4, x in the L2
+//   4096 x 11008, batch 1                      10.6          14.6              19.7
+//   11008 x 4096, batch 1                      10.2          11.8              11.3
+//   11008 x 4096, batch 8                      13.6             -              11.3
+//   the same, groups of 32 with zero points    13.9             -              14.5
+//   12288 x 2048, batch 4                      10.1           9.5               7.7
+//   9216 x 5120, batch 16                      28.7             -              13.0
+//   6144 x 2048, batch 1                        8.0           6.8               8.0
+//   16384 x 8192, batch 1                      18.5          18.3              19.4
+//   16384 x 8192, batch 16                     38.0             -              20.7
 struct Q4Plan {
     uint32_t blocks;  // of rows, a tile: 1, 2 or 4
     bool x_lds;
@@ -473,16 +476,16 @@ static Q4Plan q4_plan(const sgdrc_q4 *q, uint32_t batch, uint32_t allowed)
 {
     const uint32_t segs = (q->cols + 127u) / 128u;
     const uint64_t row_blocks = ((uint64_t)q->rows + 15u) / 16u, cus = std::max(allowed, 1u);
+    const uint64_t run = (segs + kQ4Waves - 1u) / kQ4Waves;
     const bool fits = (uint64_t)segs * 256u * batch <= kQ4XLds;
-    if (segs <= (uint32_t)kQ4Waves && row_blocks >= 2u * cus)
+    const auto rounds = [&](uint64_t blocks) { return (row_blocks + blocks * cus - 1u) / (blocks * cus); };
+    const uint64_t one = rounds(1u) * ((run + 3u) / 4u) * (8u + batch);
+    const uint64_t two = fits ? rounds(2u) * ((run + 1u) / 2u) * (9u + batch) : ~0ull;
+    const uint64_t four = rounds(4u) * (run * (q->zeros ? 9u : 8u) + 1u);
+    if (four < one && four < two)
         return {4u, false};
-    if (row_blocks > 3u * cus) {
-        if (fits && batch <= 2u && row_blocks <= 8u * cus)
-            return {2u, true};
-        return {4u, false};
-    }
-    if (batch > 4u && 2u * row_blocks >= 5u * cus)
-        return {4u, false};
+    if (two < one)
+        return {2u, true};
     return {1u, fits};
 }
 
