@@ -119,11 +119,11 @@ __device__ __forceinline__ double wave_scan(double v, uint32_t lane)
 // in and goes through that one again.  Few requests have several workgroups each: all walk
 // as far as the first sum, share its chunks, and the last to have its part
 // goes on alone (a chain needs no other sum).  N: elements of a load (1 for a vocabulary
-// below a vector's).
+// below a vector's); DRAWN: with draft rows.
 // Bound by the chain of its trips to memory (a chain of 5 over 32000: 12 us with the launch; 32 trees of up to
 // 48 certain choices over 50257: 26, a row's sum by one workgroup at each node that rejects),
 // with many long rows by the pass over them (64 chains of 8 over 131072, 67 MB: 22).
-template <int DT, uint32_t N>
+template <int DT, uint32_t N, bool DRAWN>
 __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_draft_verify(
     VerifyArgs a, uint32_t n_tiles, Gate g)
 {
@@ -134,7 +134,6 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
     __shared__ double s_chunk[kMaxChunks];
     __shared__ uint32_t s_last;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool drawn = a.draft != nullptr;
     const uint32_t n_chunks = (a.vocab + a.chunk - 1u) / a.chunk;
 
     auto body = [&](uint32_t tile, uint32_t &err) {
@@ -165,7 +164,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
             s_par[i] = par;
             s_u[i] = a.uniform[q0 + i];
             s_p[i] = in && i ? counts(row_at<DT>(a.target + row * a.target_stride, tok)) : 0.0f;
-            s_q[i] = !drawn ? 1.0f : in && i ? counts(row_at<DT>(a.draft + row * a.draft_stride, tok)) : 0.0f;
+            s_q[i] = !DRAWN ? 1.0f : in && i ? counts(row_at<DT>(a.draft + row * a.draft_stride, tok)) : 0.0f;
         }
         __syncthreads();
         int32_t par[SGDRC_MAX_NODES / 64];  // of nodes 64 k + lane
@@ -181,7 +180,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
         bool alone = a.parts == 1u, mine = n ? true : part == 0u;  // no part to share; ours is the request's end
         auto rows = [&](const uint8_t *&p, const uint8_t *&q) {
             p = a.target + (uint64_t)(q0 + cur) * a.target_stride;
-            q = drawn ? a.draft + (uint64_t)(q0 + cur) * a.draft_stride : p;
+            q = DRAWN ? a.draft + (uint64_t)(q0 + cur) * a.draft_stride : p;
         };
         auto gone = [&](uint32_t t) {
             bool x = false;
@@ -202,7 +201,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
             }
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e)
-                w[e] = drawn ? fmax((double)fp[e] - c * (double)fq[e], 0.0) : (double)fp[e];
+                w[e] = DRAWN ? fmax((double)fp[e] - c * (double)fq[e], 0.0) : (double)fp[e];
             if (ex) {
                 const uint32_t at = i - row_skip<N>(i, a.vocab);
                 for (uint32_t k = 0; k < n_ex; ++k) {
@@ -233,7 +232,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
                     const uint32_t i = i0 + (k * 64u + lane) * N;
                     vp[b][k] = row_load<DT, N>(p, i, a.vocab);
                     vq[b][k] = u32x4{0u, 0u, 0u, 0u};
-                    if (drawn)
+                    if (DRAWN)
                         vq[b][k] = row_load<DT, N>(q, i, a.vocab);
                 }
             };
@@ -353,7 +352,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
                     continue;
                 }
                 const double q = s_q[child];
-                double w = fmax((double)s_p[child] - (drawn ? c * q : 0.0), 0.0);
+                double w = fmax((double)s_p[child] - (DRAWN ? c * q : 0.0), 0.0);
                 if (gone(t))
                     w = 0.0;
                 const bool yes = w > 0.0 && (double)s_u[child] * q * left < w;
@@ -368,7 +367,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
                     summed = false;
                     continue;
                 }
-                if (drawn) {
+                if (DRAWN) {
                     c += left;
                 } else {
                     __syncthreads();
@@ -421,7 +420,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
                         double x[N];
                         const uint32_t i = i0 + lane * 16u + k * N;
                         const u32x4 vp = row_load<DT, N>(p, i, a.vocab);
-                        weights(vp, drawn ? row_load<DT, N>(q, i, a.vocab) : vp, i, ex, true, x);
+                        weights(vp, DRAWN ? row_load<DT, N>(q, i, a.vocab) : vp, i, ex, true, x);
 #pragma unroll
                         for (uint32_t e = 0; e < N; ++e)
                             w[k * N + e] = x[e];
@@ -465,10 +464,10 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
     single_tile_loop(g, n_tiles, NoOp(), body);
 }
 
-template <int DT, uint32_t N>
+template <int DT, uint32_t N, bool DRAWN>
 static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void *stream)
 {
-    static const int occ = occupancy(k_draft_verify<DT, N>, kVerifyThreads);
+    static const int occ = occupancy(k_draft_verify<DT, N, DRAWN>, kVerifyThreads);
     const uint64_t pieces = ((uint64_t)a.vocab + kSpan<DT> - 1u) / kSpan<DT>;
     const uint64_t in_chunk = (pieces + kMaxChunks - 1u) / kMaxChunks;
     a.chunk = (uint32_t)in_chunk * kSpan<DT>;
@@ -493,7 +492,7 @@ static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void
     a.sums = place;
     a.arrived = reinterpret_cast<uint32_t *>(place + kVerifySums);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL((k_draft_verify<DT, N>), dim3(gated_grid(c, occ, tiles, li)), dim3(kVerifyThreads), 0, s, a,
+    hipLaunchKernelGGL((k_draft_verify<DT, N, DRAWN>), dim3(gated_grid(c, occ, tiles, li)), dim3(kVerifyThreads), 0, s, a,
                        (uint32_t)tiles, g);
     SGDRC_HIP(hipGetLastError());
     return finish_static_tlog(g, s);
@@ -502,8 +501,11 @@ static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void
 template <int DT>
 static int launch_verify_size(sgdrc_ctx *ctx, const VerifyArgs &a, uint32_t n_requests, void *stream)
 {
-    return a.vocab < kVec<DT> ? launch_verify<DT, 1>(ctx, a, n_requests, stream)
-                              : launch_verify<DT, kVec<DT>>(ctx, a, n_requests, stream);
+    if (a.vocab < kVec<DT>)
+        return a.draft ? launch_verify<DT, 1, true>(ctx, a, n_requests, stream)
+                       : launch_verify<DT, 1, false>(ctx, a, n_requests, stream);
+    return a.draft ? launch_verify<DT, kVec<DT>, true>(ctx, a, n_requests, stream)
+                   : launch_verify<DT, kVec<DT>, false>(ctx, a, n_requests, stream);
 }
 
 }  // namespace sgdrc
