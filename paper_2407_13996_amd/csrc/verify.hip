@@ -35,8 +35,7 @@ template <int DT>
 constexpr uint32_t kVec = DT == SGDRC_F32 ? 4u : 8u;
 
 // Elements that a wavefront sums at once.
-template <int DT>
-constexpr uint32_t kSpan = DT == SGDRC_F32 ? 1024u : 2048u;
+constexpr uint32_t kSpan = 1024u;
 
 template <int DT>
 constexpr uint32_t kSize = DT == SGDRC_F32 ? 4u : 2u;
@@ -73,9 +72,37 @@ __device__ __forceinline__ uint32_t row_skip(uint32_t i, uint32_t vocab)
     return i - min(i, vocab - N);
 }
 
-// The probabilities in them, as they count.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// The largest bit patterns seen, of whole words (fp32) or of both halves: up to
+// row_plain's they are numbers that count as they are, without the clamps.
+template <int DT>
+__device__ __forceinline__ uint32_t row_top(uint32_t top, u32x4 v)
+{
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (DT == SGDRC_F32)
+            top = max(top, x[e]);
+        else
+            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                                         __builtin_bit_cast(u16x2, x[e])));
+    }
+    return top;
+}
+
+template <int DT>
+__device__ __forceinline__ bool row_plain(uint32_t top)
+{
+    if (DT == SGDRC_F32)
+        return top <= 0x7F7FFFFFu;
+    const uint32_t most = DT == SGDRC_BF16 ? 0x7F7Fu : 0x7BFFu;
+    return (top & 0xFFFFu) <= most && top >> 16 <= most;
+}
+
+// The probabilities in them, as they count (``plain``: as they are).
 template <int DT, uint32_t N>
-__device__ __forceinline__ void row_floats(u32x4 v, float (&f)[N])
+__device__ __forceinline__ void row_floats(u32x4 v, float (&f)[N], bool plain = false)
 {
     const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -88,7 +115,8 @@ __device__ __forceinline__ void row_floats(u32x4 v, float (&f)[N])
             const f16x2 h = __builtin_bit_cast(f16x2, x[e / 2u]);
             f[e] = e % 2u ? (float)h.y : (float)h.x;
         }
-        f[e] = counts(f[e]);
+        if (!plain)
+            f[e] = counts(f[e]);
     }
 }
 
@@ -120,14 +148,15 @@ __device__ __forceinline__ double wave_scan(double v, uint32_t lane)
 // as far as the first sum, share its chunks, and the last to have its part
 // goes on alone (a chain needs no other sum).  N: elements of a load (1 for a vocabulary
 // below a vector's); DRAWN: with draft rows.
-// Bound by the chain of its trips to memory (a chain of 5 over 32000: 12 us with the launch; 32 trees of up to
-// 48 certain choices over 50257: 26, a row's sum by one workgroup at each node that rejects),
-// with many long rows by the pass over them (64 chains of 8 over 131072, 67 MB: 22).
+// Bound by the chain of its trips to memory (a chain of 5 over 32000: 10.5 us with the launch; 32 trees of up to
+// 48 certain choices over 50257: 19.6, a row's sum by one workgroup at each node that rejects),
+// with many long rows by the pass over them and its 64-bit arithmetic (64 chains of 8 over 131072, 67 MB: 20).
+// Spans of 2048 16-bit elements take 22.7 for the trees, two spans ahead 20.2, 1024 threads 27.
 template <int DT, uint32_t N, bool DRAWN>
 __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_draft_verify(
     VerifyArgs a, uint32_t n_tiles, Gate g)
 {
-    constexpr uint32_t kLoads = N == 1u ? 1u : kSpan<DT> / 64u / N;
+    constexpr uint32_t kLoads = N == 1u ? 1u : kSpan / 64u / N;
     __shared__ int32_t s_tok[SGDRC_MAX_NODES], s_par[SGDRC_MAX_NODES], s_path[SGDRC_MAX_NODES];
     __shared__ float s_u[SGDRC_MAX_NODES], s_p[SGDRC_MAX_NODES], s_q[SGDRC_MAX_NODES];
     __shared__ uint32_t s_ex[SGDRC_MAX_NODES];  // tokens ruled out at the node (without draft rows)
@@ -221,7 +250,7 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
         };
         // The sums of chunks ``from``, from + by, ... below ``end``: a span's loads go out
         // together, before the one that came before them is summed.
-        const uint32_t per = a.chunk / kSpan<DT>;  // spans of a chunk
+        const uint32_t per = a.chunk / kSpan;  // spans of a chunk
         auto sum_chunks = [&](uint32_t from, uint32_t end, uint32_t by) __attribute__((always_inline)) {
             const uint8_t *p, *q;
             rows(p, q);
@@ -247,20 +276,39 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
                 for (int b = 0; b < 2; ++b) {
                     if (!more)
                         break;
-                    const uint32_t at = ch * a.chunk + j * kSpan<DT>;
-                    const bool odd = at + kSpan<DT> > a.vocab;
+                    const uint32_t at = ch * a.chunk + j * kSpan;
+                    const bool odd = at + kSpan > a.vocab;
                     const bool last = j + 1u == per;
                     const uint32_t ch2 = last ? ch + by : ch, j2 = last ? 0u : j + 1u;
                     more = ch2 < end;
-                    if (more)
-                        fetch(ch2 * a.chunk + j2 * kSpan<DT>, b ^ 1);
+                    // (always: the loads before would be waited for where one may be missing)
+                    fetch(more ? ch2 * a.chunk + j2 * kSpan : at, b ^ 1);
+                    uint32_t top = 0u;
 #pragma unroll
                     for (uint32_t k = 0; k < kLoads; ++k) {
-                        double w[N];
-                        weights(vp[b][k], vq[b][k], at + (k * 64u + lane) * N, ex, odd, w);
+                        top = row_top<DT>(top, vp[b][k]);
+                        if (DRAWN)
+                            top = row_top<DT>(top, vq[b][k]);
+                    }
+                    if (N > 1 && !ex && !odd && __ballot(!row_plain<DT>(top)) == 0ull) {
 #pragma unroll
-                        for (uint32_t e = 0; e < N; ++e)
-                            sum += w[e];
+                        for (uint32_t k = 0; k < kLoads; ++k) {
+                            float fp[N], fq[N];
+                            row_floats<DT, N>(vp[b][k], fp, true);
+                            row_floats<DT, N>(vq[b][k], fq, true);
+#pragma unroll
+                            for (uint32_t e = 0; e < N; ++e)
+                                sum += DRAWN ? fmax((double)fp[e] - c * (double)fq[e], 0.0) : (double)fp[e];
+                        }
+                    } else {
+#pragma unroll
+                        for (uint32_t k = 0; k < kLoads; ++k) {
+                            double w[N];
+                            weights(vp[b][k], vq[b][k], at + (k * 64u + lane) * N, ex, odd, w);
+#pragma unroll
+                            for (uint32_t e = 0; e < N; ++e)
+                                sum += w[e];
+                        }
                     }
                     if (last) {
                         sum = wave_sum(sum);
@@ -468,9 +516,9 @@ template <int DT, uint32_t N, bool DRAWN>
 static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void *stream)
 {
     static const int occ = occupancy(k_draft_verify<DT, N, DRAWN>, kVerifyThreads);
-    const uint64_t pieces = ((uint64_t)a.vocab + kSpan<DT> - 1u) / kSpan<DT>;
+    const uint64_t pieces = ((uint64_t)a.vocab + kSpan - 1u) / kSpan;
     const uint64_t in_chunk = (pieces + kMaxChunks - 1u) / kMaxChunks;
-    a.chunk = (uint32_t)in_chunk * kSpan<DT>;
+    a.chunk = (uint32_t)in_chunk * kSpan;
     const uint32_t chunks = (uint32_t)((pieces + in_chunk - 1u) / in_chunk);
     Ctx *c = nullptr;
     int rc = check_ctx(ctx, &c);
@@ -478,7 +526,7 @@ static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void
         return rc;
     // Workgroups of a request: one a CU over all requests, each wavefront with a
     // chunk, sums that fit the stream's place for them.  (Chains of 8 nodes over 131072
-    // float values, 64 of them: 22 us, two workgroups a CU 31, without parts 37.  One: 13 and 30.)
+    // float values, 64 of them: 20 us, two workgroups a CU 19.3, without parts 28.  One: 11.4 and 22.)
     a.parts = 1u;
     if (n_requests <= kVerifyShared && (uint64_t)n_requests * chunks <= kVerifySums)
         a.parts = std::max(1u, std::min({16u, (uint32_t)stream_allowed_cus(c, stream) / n_requests,

@@ -308,3 +308,22 @@ def test_rows_shared_by_workgroups(ctx, dtype):
         s.synchronize()
         compare(ctx, outs[0], args[0], None, *args[2:], path_stride=16)
     sg.stream_release(ctx, s)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_odd_probabilities_among_many(ctx, dtype, drawn):
+    """One element in a thousand is NaN, infinite, negative, -0 or the smallest there is, so that some
+    runs of a row hold such elements and others none; an infinity counts as the largest fp32 and
+    leaves the draw to itself, so that most rows have none."""
+    target, guess, tokens, parents, u, q_start = case([7, 5, 30, 1, 12, 9], 20011, "tree", dtype, 60)
+    g = torch.Generator().manual_seed(61)
+    least = torch.tensor([1], dtype=torch.int32 if dtype == "f32" else torch.int16).view(TYPES[dtype])[0].item()
+    for t in (target, guess):
+        n = t.numel() // 1000
+        at = torch.randperm(t.numel(), generator=g)[:n]
+        odd = torch.tensor([float("nan"), -0.5, -0.0, least, float("-inf"), -float("nan")], dtype=t.dtype)
+        t.view(-1)[at] = odd[torch.randint(0, len(odd), (n,), generator=g)]
+    target[3, 15000] = target[40, 3] = guess[20, 777] = float("inf")
+    got = call(ctx, target.to(DEV), guess.to(DEV) if drawn else None, tokens, parents, u, q_start)
+    compare(ctx, got, target, guess if drawn else None, tokens, parents, u, q_start)
