@@ -25,7 +25,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr int kQ4Threads = 512;
 constexpr int kQ4Waves = kQ4Threads / 64;
 constexpr uint32_t kQ4Block = 1024;        // bytes of a block of codes, 16 rows by 128 columns
-constexpr uint32_t kQ4Outside = 0xFFFFFFF0u;  // an offset past any buffer resource
+constexpr uint32_t kQ4Outside = 0xC0000000u;  // past x (2 MiB at most), with any column's offset added too
+                                              // (as the bits of -2.0f an instruction's own constant, no register)
 
 struct Q4View {
     const uint8_t *pool;
