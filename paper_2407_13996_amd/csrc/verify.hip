@@ -437,14 +437,14 @@ __global__ __launch_bounds__(kVerifyThreads) __attribute__((amdgpu_waves_per_eu(
             // The chunk that the goal falls in, of which a lane holds 8.  (Where rounding
             // leaves the goal above all sums: the last that holds anything.)
             constexpr uint32_t kHeld = kMaxChunks / 64u;
-            double mine = 0.0;
+            double held = 0.0;
             for (uint32_t k = 0; k < kHeld; ++k)
-                mine += lane * kHeld + k < n_chunks ? s_chunk[lane * kHeld + k] : 0.0;
-            const double upto = wave_scan(mine, lane);
-            const uint64_t past = __ballot(mine > 0.0 && upto > goal), some = __ballot(mine > 0.0);
+                held += lane * kHeld + k < n_chunks ? s_chunk[lane * kHeld + k] : 0.0;
+            const double upto = wave_scan(held, lane);
+            const uint64_t past = __ballot(held > 0.0 && upto > goal), some = __ballot(held > 0.0);
             if (some) {
                 const uint32_t l = past ? (uint32_t)__builtin_ctzll(past) : 63u - (uint32_t)__builtin_clzll(some);
-                double before = __shfl(upto - mine, l, 64), run = before;
+                double before = __shfl(upto - held, l, 64), run = before;
                 uint32_t ch = 0u;
                 bool found = false;
                 for (uint32_t k = 0; k < kHeld; ++k) {
@@ -526,7 +526,8 @@ static int launch_verify(sgdrc_ctx *ctx, VerifyArgs a, uint32_t n_requests, void
         return rc;
     // Workgroups of a request: one a CU over all requests, each wavefront with a
     // chunk, sums that fit the stream's place for them.  (Chains of 8 nodes over 131072
-    // float values, 64 of them: 20 us, two workgroups a CU 19.3, without parts 28.  One: 11.4 and 22.)
+    // float values, 64 of them: 20.4 us, two workgroups a CU 20.7, without parts 32.3.  One
+    // chain: 11.3 either way, without parts 22.4.)
     a.parts = 1u;
     if (n_requests <= kVerifyShared && (uint64_t)n_requests * chunks <= kVerifySums)
         a.parts = std::max(1u, std::min({16u, (uint32_t)stream_allowed_cus(c, stream) / n_requests,
