@@ -655,7 +655,8 @@ int colored_kv_append(sgdrc_ctx *ctx, const sgdrc_kv_cache *cache, uint32_t laye
 
 /* What happens to queries and keys on their way to the attention.  A head h
  * becomes h * rsqrt(mean(h^2) + eps) * w, element by element, if weights w are
- * given (head_dim of them, of norm_dtype; q and k each have their own or none).
+ * given (head_dim of them, of norm_dtype; q and k each have their own or none; the sum
+ * of a head's squares must be a number of fp32's range).
  * Then its first rot_dims dimensions turn in pairs, by the angle position * freq[i] radians
  * for pair i: (a, b) -> (a cos - b sin, a sin + b cos).  Pair i is
  * dimensions (i, i + rot_dims / 2), or (2 i, 2 i + 1) if interleaved. */
@@ -776,7 +777,10 @@ int sgdrc_tree_attention_workspace(const sgdrc_kv_cache *cache, uint32_t n_heads
  * left the next token is drawn from what is left there: the first v at which the
  * running sum of max(p - c q, 0) passes u_0 times its total, u_0 the root's
  * random number (from p itself, if nothing is left).  So the tokens are
- * distributed as if drawn from the target alone.
+ * distributed as if drawn from the target alone, where the rows sum to 1: a node's
+ * first child is compared with p and q as they are, not with parts of their sums, so
+ * that rows of which only the best tokens were kept have to be scaled to 1 again (rows
+ * rounded to 16 bits are off by as much as their sums are).
  * Sums are held in 64 bits.  Probabilities that are not positive (NaN too)
  * count as 0, infinite ones as the largest fp32.  Random numbers lie in [0, 1); with
  * others a token is chosen all the same.  A node whose token is outside the

@@ -692,8 +692,8 @@ def colored_draft_verify(ctx, target, tokens, parents, uniform, q_start, path, a
                          totals=None, max_nodes: int = 256, stream=None) -> None:
     """Which nodes of each request's tree a sampler of the target would have taken
     (``path`` [requests, most], -1 past the ``accepted`` first) and its ``next`` token.
-    ``target`` and ``draft`` [tokens, vocab]: probabilities after each node, and those that
-    its children were drawn from (None: certain choices); ``tokens``, ``parents`` (in
+    ``target`` and ``draft`` [tokens, vocab]: probabilities after each node (rows that sum to 1: cut ones scaled
+    again), and those that its children were drawn from (None: certain choices); ``tokens``, ``parents`` (in
     the request's own count) and ``uniform`` (fp32, [0, 1)): an entry a node, the root's random
     number is the next token's.  ``lens``, ``totals``: as for the attention; a
     request that was not served accepts nothing.  path, accepted and lens, totals go on to colored_kv_commit."""
