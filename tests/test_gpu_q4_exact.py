@@ -158,3 +158,15 @@ def test_columns_past_4_gib(ctx):
         got = y[:, t * 16:t * 16 + 16]
         assert torch.equal(got, w[:, :got.shape[1]])
     assert ctx.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype,x_to,s_to", [(sg.F16, -24, 0), (sg.F16, 0, -23), (sg.BF16, -133, 0), (sg.BF16, 0, -126)])
+def test_denormal_numbers_count(ctx, dtype, x_to, s_to):
+    """x or the scales at the smallest that their type has: nothing is taken for zero."""
+    for rows, cols, batch in ((100, 1024, 3), (5120, 5376, 1), (11008, 4096, 8)):
+        m = whole(rows, cols, 64, dtype, True, 14, seed=5)
+        m.scales = (m.scales.double() * 2.0 ** s_to).to(DT[dtype])
+        m.upload(ctx)
+        x = (numbers(batch, cols, dtype, 1).double() * 2.0 ** x_to).to(DT[dtype])
+        assert bool((x != 0).all()) and bool((m.scales != 0).all())
+        assert torch.equal(product(ctx, m, x).double(), exact(m, x)), (rows, cols, batch)
