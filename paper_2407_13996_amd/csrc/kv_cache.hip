@@ -289,8 +289,8 @@ constexpr uint32_t kCommitBatch = 8;  // path entries whose loads are in flight 
 // several entries before it stores any.  Bound by the scattered accesses that the
 // layout asks for: a token's K is 16 bytes every 16 block_tokens, its V 2 bytes
 // in every 16.  64 requests of 32 layers and 8 heads of 128 that keep 6 of 60
-// tokens take 109 us, K and V half each; for 42 MB moved the L2 reads 2.1 million
-// times from memory (267 MB by its 128-byte lines) and writes 91 MB, 3.3 TB/s
+// tokens take 109 us, K and V half each; for 42 MB moved the L2 reads 2.0 million
+// times from memory (257 MB by its 128-byte lines) and writes 91 MB, 3.2 TB/s
 // together.  (Whole 16-byte groups of V, read and written again, took 104, and would
 // rewrite tokens that are not this call's.)
 template <int D>

@@ -453,19 +453,21 @@ typedef void (*Q4Kernel)(Q4View, const uint32_t *, const uint8_t *, uint32_t, ui
 // other or side by side.  A unit with one row block loads x for four segments, with
 // four blocks for one, which all blocks share; what it costs grows with the rows of x that
 // come out of LDS or the L2, while four blocks cost their codes, and more with zero points.  The form with the
-// least cost, in the weights below, is the best of the three in time but for 0.2 to 1.2 % on average
-// (at worst 19) over 1100 measured calls: all groups, with and without zero points, 2048 to 65536 rows,
-// 1024 to 11008 columns, batches 1 to 16, rotated copies.  bf16, 2 MiB pages, groups of 64, us:
+// least cost, in the weights below, is slower than the best of the three by 0.2 to 1.2 % on average
+// over each kind of matrix and by 17 % at worst, over 1100 measured calls: all groups, with and without zero points,
+// 2048 to 65536 rows, 1024 to 11008 columns, batches 1 to 16.  The weights do not
+// know the groups' size; in the lines marked * they take the slower form.
+// bf16, 2 MiB pages, groups of 64, copies in turn (400 MB or 10 of them), us:
 //                                                 1    2, x in LDS    4, x in the L2
-//   4096 x 11008, batch 1                      10.6          14.6              19.7
-//   11008 x 4096, batch 1                      10.2          11.8              11.3
-//   11008 x 4096, batch 8                      13.6             -              11.3
-//   the same, groups of 32 with zero points    13.9             -              14.5
-//   12288 x 2048, batch 4                      10.1           9.5               7.7
-//   9216 x 5120, batch 16                      28.7             -              13.0
-//   6144 x 2048, batch 1                        8.0           6.8               8.0
-//   16384 x 8192, batch 1                      18.5          18.3              19.4
-//   16384 x 8192, batch 16                     38.0             -              20.7
+//   4096 x 11008, batch 1                      10.5          14.4              19.6
+//   11008 x 4096, batch 1                      10.1          11.8              11.1
+//   11008 x 4096, batch 8                      13.7             -              11.4
+//   the same, groups of 32 with zero points    13.9             -              14.6  *
+//   12288 x 2048, batch 4                      10.2           9.5               8.0
+//   9216 x 5120, batch 16                      28.7             -              13.1
+//   6144 x 2048, batch 1                        8.0           6.8               7.8
+//   16384 x 8192, batch 1                      18.8          18.4              19.8  *
+//   16384 x 8192, batch 16                     37.8             -              21.1
 struct Q4Plan {
     uint32_t blocks;  // of rows, a tile: 1, 2 or 4
     bool x_lds;

@@ -197,7 +197,10 @@ __device__ __forceinline__ void turn_angle(int32_t position, float freq, float &
 // that no load queues behind a store.  Values: as in k_kv_append.
 //
 // 16384 tokens of 32 + 8 + 8 heads of 128, 403 MB: 91 us on MI355X (4.5 TB/s), without norms and
-// rotation too: the movement bounds it, in pieces of 128 bytes; U = 2 reloaded one by
+// rotation too: the movement in this shape bounds it.  A load or store of a wavefront takes 128 bytes of each of
+// eight rows, the other halves come by a second one, as a lane's two pieces lie half a
+// rotation apart (lanes side by side over whole rows, with a pair's partners
+// in other lanes, have not been measured).  U = 2 reloaded one by
 // one, four workgroups a CU, 104; U = 8, two workgroups, 102; U = 4, four workgroups, with
 // spilled registers, 110; a token's heads side by side, its angles by way of LDS, 114.
 template <int DT, int D, int TOKENS>
